@@ -381,6 +381,87 @@ int cmoe_token_permute_static(const int32_t* topk_idx, int32_t n_rows, int32_t n
                               int32_t n_groups, int32_t* counts, int32_t* offsets,
                               int32_t* row_token, int32_t* row_of, void* stream);
 
+/* ---- Low-rank adapters and dropout (fine-tuning of the restructured model, Section 5.1: low-rank adapters of rank 8
+ * with alpha 32; and serving many fine-tunes of one set of weights). ----
+ *
+ * Dropout by a counter-based generator: whether an element is kept is a function of (seed, offset, row, column) alone, so
+ * no mask is stored, and a backward pass, a second device or a part of the batch gets the same mask.
+ *   Columns 8 c .. 8 c + 7 of row t share one block of Philox 4x32-10 (Salmon et al. 2011) on the counter words
+ *   (c, row0 + t, offset mod 2^32, offset / 2^32) under the key words (seed mod 2^32, seed / 2^32); column 8 c + j takes the
+ *   16-bit half j of the block (word j / 2, the low half first) and is kept where that number is at least
+ *   thr = floor(65536 p + 0.5).  Kept elements are scaled by 65536 / (65536 - thr): p is held to 1 / 65536, with an exact mean.
+ *   p      : 0 <= p < 1 - 2^-17.   row0 >= 0, row0 + rows <= 2^32: rows of a batch that is processed in parts.
+ * Use a new (seed, offset) for every mask that has to be independent of the others. */
+typedef struct {
+  double p;
+  uint64_t seed, offset;
+  int64_t row0;
+} cmoe_dropout_config;
+
+/* out[t, c] = residual[t, c] + keep(t, c) * x[t, c] / (1 - p); a dropped element contributes 0 even where x is NaN or Inf.
+ * The gradient by x is the same call on the output's gradient without a residual; that by the residual is the gradient itself.
+ *   x, residual (NULL: zero), out: device, [rows, cols] with row strides ldx, ld_residual, ld_out >= cols in elements, of
+ *   dtype (cmoe_dtype).  out may be x or residual (same pointer and stride); otherwise it overlaps neither.  Any width,
+ *   stride and element-aligned pointer; rows that start on 16-byte boundaries are faster.  Elements outside the matrix
+ *   are not written.  Sums and scale in fp32, rounded once.
+ * Asynchronous on `stream`, one launch, allocates nothing; rows == 0 or cols == 0 is a no-op.  Errors: INVALID_ARG, CUDA, UNSUPPORTED. */
+int cmoe_dropout(const void* x, int64_t ldx, const void* residual, int64_t ld_residual, int32_t rows, int32_t cols, int32_t dtype,
+                 const cmoe_dropout_config* drop, void* out, int64_t ld_out, void* stream);
+
+/* A set of low-rank adapters of one projection [d_in] -> [d_out].
+ *   a : device, [n_adapters, rank, d_in]; b : device, [n_adapters, d_out, rank]; both contiguous, 16-byte aligned, of dtype.
+ *   scale : device float [n_adapters] (alpha / rank of each) or NULL (1).
+ *   1 <= n_adapters <= 1024; rank a multiple of 8, at most 64 (adapters of other ranks are padded with zeros, which
+ *   changes no result); d_in, d_out multiples of 8, at most 2^24.  Weights are taken to be finite.
+ * The struct is read during the call; the arrays belong to the caller. */
+typedef struct {
+  int32_t n_adapters, rank, d_in, d_out, dtype;
+  const void *a, *b;
+  const float* scale;
+} cmoe_adapters;
+
+/* Scratch that the calls below need for n_rows rows (256-byte aligned; contents need not be initialised).  row_adapter
+ * given (1) or NULL (0); backward: 1 for cmoe_adapter_backward.  0 for arguments that the calls refuse. */
+int64_t cmoe_adapter_scratch_bytes(const cmoe_adapters* ad, int32_t n_rows, int32_t with_row_adapter, int32_t backward);
+
+/* out_t = base_t + s_a B_a (A_a xd_t) for every row t with its own adapter a = row_adapter[t]; a number outside
+ * [0, n_adapters) means no adapter: out_t = base_t.  xd is x, or its dropout by `drop` (NULL: none).
+ *   x    : device, [n_rows, d_in], row stride ldx;  base : device, [n_rows, d_out], row stride ld_base, or NULL (zero): what the
+ *          shared projection gave for the rows;  out : device, [n_rows, d_out], row stride ld_out; may be base (same pointer
+ *          and stride), overlaps neither x nor base otherwise.  Strides in elements, at least the width; pointers and strides
+ *          are multiples of 16 bytes.  Rows of other matrices may lie between (column slices of a wider one).
+ *   row_adapter : device int32 [n_rows], in any order, or NULL: every row takes adapter 0.
+ *   z    : device float [n_rows, rank] or NULL; receives A_a xd_t (zeros for rows without an adapter), for the backward pass.
+ *   scratch : needed where row_adapter is given and n_rows > 256.
+ * Products with fp32 sums (bf16: the narrow middle keeps at least 15 significant bits), rounded once.  A row's result does
+ * not depend on the other rows' values.  Asynchronous on `stream`, one launch (two with scratch), allocates nothing;
+ * n_rows == 0 is a no-op.  Two calls that may overlap in time (other streams, captured graphs) need a scratch each.
+ * Errors: INVALID_ARG, CAPACITY (scratch too small, n_rows above 2^30), CUDA, UNSUPPORTED. */
+int cmoe_adapter_forward(const cmoe_adapters* ad, const void* x, int64_t ldx, const int32_t* row_adapter, int32_t n_rows,
+                         const cmoe_dropout_config* drop, const void* base, int64_t ld_base, void* out, int64_t ld_out, float* z,
+                         void* scratch, int64_t scratch_bytes, void* stream);
+
+/* Gradients of cmoe_adapter_forward for dout = dy, with the forward's x, z, row_adapter and drop:
+ *   e_t = s_a B_a^T dy_t,  dx_t = dx_base_t + m_t * (A_a^T e_t),  grad_a[a] = sum_t e_t xd_t^T,  grad_b[a] = sum_t s_a dy_t z_t^T
+ * (m_t: the mask with its scale; sums over the rows of adapter a).
+ *   dy : device, [n_rows, d_out];  dx_base : device, [n_rows, d_in] or NULL (zero), e.g. the projection's own dx;
+ *   dx : device, [n_rows, d_in], may be dx_base, or NULL: not wanted.
+ *   grad_a [n_adapters, rank, d_in], grad_b [n_adapters, d_out, rank]: device, in the adapters' dtype, 16-byte aligned, written
+ *   whole (zeros for adapters without rows), or both NULL: not wanted, then x and z may be NULL.  Sums in fp32 over the rows in
+ *   a fixed order: the same call gives the same bits.
+ * n_rows == 0 zeroes the gradients of the weights.  Scratch is always needed for n_rows > 0.  Otherwise as the forward. */
+int cmoe_adapter_backward(const cmoe_adapters* ad, const void* dy, int64_t ld_dy, const void* x, int64_t ldx, const float* z,
+                          const int32_t* row_adapter, int32_t n_rows, const cmoe_dropout_config* drop, const void* dx_base,
+                          int64_t ld_dx_base, void* dx, int64_t ld_dx, void* grad_a, void* grad_b, void* scratch,
+                          int64_t scratch_bytes, void* stream);
+
+/* out_t = F_MoE(x_t) + s_a B_a A_a x_t: cmoe_ffn_forward with an adapter per request beside the layer, which all of them share.
+ * The adapters' d_in and d_out are the layer's d_model and their dtype is the layer's; x, T, out as in cmoe_ffn_forward,
+ * row_adapter, scratch as in cmoe_adapter_forward.  Arguments are checked before anything is launched.  The adapters are not
+ * part of the per-stage times; cmoe_layer_launch_count includes their launches.  Errors: those of both calls. */
+int cmoe_ffn_forward_adapted(cmoe_layer* layer, const void* x, int32_t T, const cmoe_adapters* ad, const int32_t* row_adapter,
+                             void* out, void* scratch, int64_t scratch_bytes, void* stream);
+
 const char* cmoe_status_string(int status);
 /* Text of the most recent error seen by this library on the calling thread. */
 const char* cmoe_last_error(void);

@@ -6,7 +6,8 @@ from __future__ import annotations
 
 import ctypes as C
 import os
-from typing import Dict, Optional, Sequence
+from contextlib import nullcontext
+from typing import Dict, NamedTuple, Optional, Sequence
 
 import numpy as np
 
@@ -27,6 +28,7 @@ EXPORTS = [
     "cmoe_layer_launch_count", "cmoe_layer_gemm_forms", "cmoe_layer_enable_stage_timing", "cmoe_layer_stage_times",
     "cmoe_layer_destroy", "cmoe_token_permute_scratch_bytes",
     "cmoe_token_permute", "cmoe_token_permute_static", "cmoe_status_string", "cmoe_last_error",
+    "cmoe_dropout", "cmoe_adapter_scratch_bytes", "cmoe_adapter_forward", "cmoe_adapter_backward", "cmoe_ffn_forward_adapted",
 ]
 
 
@@ -34,6 +36,15 @@ class CmoeConfig(C.Structure):
     _fields_ = [("d_model", C.c_int32), ("d_ff", C.c_int32), ("n_experts", C.c_int32),
                 ("n_shared", C.c_int32), ("top_k", C.c_int32), ("max_tokens", C.c_int32),
                 ("dtype", C.c_int32)]
+
+
+class CmoeDropoutConfig(C.Structure):
+    _fields_ = [("p", C.c_double), ("seed", C.c_uint64), ("offset", C.c_uint64), ("row0", C.c_int64)]
+
+
+class CmoeAdapters(C.Structure):
+    _fields_ = [("n_adapters", C.c_int32), ("rank", C.c_int32), ("d_in", C.c_int32), ("d_out", C.c_int32),
+                ("dtype", C.c_int32), ("a", C.c_void_p), ("b", C.c_void_p), ("scale", C.c_void_p)]
 
 
 class CmoeError(RuntimeError):
@@ -85,6 +96,12 @@ def load() -> C.CDLL:
     lib.cmoe_token_permute_scratch_bytes.restype = i64
     lib.cmoe_token_permute.argtypes = [vp, i32, i32, i32, vp, vp, vp, vp, vp, i64, vp]
     lib.cmoe_token_permute_static.argtypes = [vp, i32, i32, i32, vp, vp, vp, vp, vp]
+    lib.cmoe_dropout.argtypes = [vp, i64, vp, i64, i32, i32, i32, vp, vp, i64, vp]
+    lib.cmoe_adapter_scratch_bytes.argtypes = [vp, i32, i32, i32]
+    lib.cmoe_adapter_scratch_bytes.restype = i64
+    lib.cmoe_adapter_forward.argtypes = [vp, vp, i64, vp, i32, vp, vp, i64, vp, i64, vp, vp, i64, vp]
+    lib.cmoe_adapter_backward.argtypes = [vp, vp, i64, vp, i64, vp, vp, i32, vp, vp, i64, vp, i64, vp, vp, vp, i64, vp]
+    lib.cmoe_ffn_forward_adapted.argtypes = [vp, vp, i32, vp, vp, vp, vp, i64, vp]
     lib.cmoe_status_string.argtypes = [C.c_int]
     lib.cmoe_status_string.restype = C.c_char_p
     lib.cmoe_last_error.restype = C.c_char_p
@@ -178,6 +195,22 @@ class Layer:
         st = load().cmoe_ffn_forward(self._h, x.data_ptr(), x.shape[0], out.data_ptr(),
                                      _stream_ptr(stream))
         _check(st, "cmoe_ffn_forward")
+        return out
+
+    def forward_adapted(self, x, a, b, row_adapter=None, scale=None, out=None, scratch=None, stream=None):
+        """cmoe_ffn_forward_adapted: the forward of x [T,d] plus the low-rank adapter of every row
+        (a, b, row_adapter, scale, scratch as in adapter_forward)."""
+        rows, d = _rows(x, "x")
+        ad = _adapters(x, a, b, scale)
+        ids = _adapter_ids(row_adapter, rows, x)
+        with _on(x, stream):
+            out = _out(out, "out", rows, d, x)
+            if d != self.d_model or not (x.is_contiguous() and out.is_contiguous()):
+                raise ValueError("x and out must be contiguous [T, d_model]")
+            scratch = _adapter_scratch(ad, rows, ids, 0, scratch, x)
+            st = load().cmoe_ffn_forward_adapted(self._h, x.data_ptr(), rows, C.byref(ad), ids, out.data_ptr(), _ptr(scratch),
+                                                 0 if scratch is None else scratch.numel(), _stream_ptr(None))
+        _check(st, "cmoe_ffn_forward_adapted")
         return out
 
     def forward_host(self, x_host, out_host, chunk_tokens: int = 0, stream=None):
@@ -406,3 +439,180 @@ def token_permute_static(topk_idx, n_groups: int, out=None, stream=None):
                                           _stream_ptr(stream))
     _check(st, "cmoe_token_permute_static")
     return counts, offsets, row_token[:n_rows * n_k], row_of
+
+
+class Dropout(NamedTuple):
+    """A dropout mask (cmoe_dropout_config): rows row0 .. of the mask named by (seed, offset), elements dropped with probability p."""
+    p: float
+    seed: int = 0
+    offset: int = 0
+    row0: int = 0
+
+
+def _drop_config(drop: Optional[Dropout]):
+    return None if drop is None else CmoeDropoutConfig(drop.p, drop.seed & 0xFFFFFFFFFFFFFFFF, drop.offset & 0xFFFFFFFFFFFFFFFF, drop.row0)
+
+
+def _rows(t, what: str):
+    """(rows, columns) of a row-strided CUDA matrix."""
+    if not t.is_cuda or t.dim() != 2:
+        raise ValueError(f"{what}: a two-dimensional CUDA tensor is expected")
+    _matrix(t, what, t.shape[0], t.shape[1], t)
+    return t.shape
+
+
+def _matrix(t, what: str, rows: int, cols: int, like) -> None:
+    """A row-strided matrix of the device and type of `like`."""
+    if t.shape != (rows, cols) or t.dtype != like.dtype or t.device != like.device or (cols > 1 and rows > 0 and t.stride(1) != 1):
+        raise ValueError(f"{what}: expected [{rows}, {cols}] of {like.dtype} on {like.device} with neighbouring columns")
+
+
+def _ld(t) -> int:
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]       # the stride of a single row has no meaning
+
+
+def _on(like, stream):
+    """A context in which the tensor's device is current and `stream` (None: that device's current one) takes the work,
+    allocations included, so that what the call frees is not handed to work of another stream."""
+    import torch
+    if stream is not None:
+        if stream.device != like.device:
+            raise ValueError("the stream and the tensors are on different devices")
+        return torch.cuda.stream(stream)
+    return nullcontext() if like.device.index == torch.cuda.current_device() else torch.cuda.device(like.device)
+
+
+def _out(out, what: str, rows: int, cols: int, like):
+    if out is None:
+        import torch
+        return torch.empty((rows, cols), dtype=like.dtype, device=like.device)
+    _matrix(out, what, rows, cols, like)
+    return out
+
+
+def dropout(x, drop: Dropout, residual=None, out=None, stream=None):
+    """cmoe_dropout on CUDA tensors [rows, cols] (rows may be strided): residual + keep * x / (1 - p).  The gradient by x is
+    dropout(dout, drop)."""
+    rows, cols = _rows(x, "x")
+    code = _dtype_code(x)
+    if residual is not None:
+        _matrix(residual, "residual", rows, cols, x)
+    cfg = _drop_config(drop)
+    with _on(x, stream):
+        out = _out(out, "out", rows, cols, x)
+        st = load().cmoe_dropout(x.data_ptr(), _ld(x), None if residual is None else residual.data_ptr(),
+                                 0 if residual is None else _ld(residual), rows, cols, code, C.byref(cfg),
+                                 out.data_ptr(), _ld(out), _stream_ptr(None))
+    _check(st, "cmoe_dropout")
+    return out
+
+
+def _adapters(like, a, b, scale) -> CmoeAdapters:
+    n, r, d_in = a.shape
+    d_out = b.shape[1]
+    for t, what, shape in ((a, "a", (n, r, d_in)), (b, "b", (n, d_out, r))):
+        if t.shape != shape or t.dtype != like.dtype or t.device != like.device or not t.is_contiguous():
+            raise ValueError(f"{what}: expected a contiguous {list(shape)} of {like.dtype} on {like.device}")
+    if scale is not None:
+        import torch
+        if scale.shape != (n,) or scale.dtype != torch.float32 or scale.device != like.device or not scale.is_contiguous():
+            raise ValueError("scale: expected a contiguous float32 tensor, one value per adapter")
+    return CmoeAdapters(n, r, d_in, d_out, _dtype_code(like), a.data_ptr(), b.data_ptr(), None if scale is None else scale.data_ptr())
+
+
+def _adapter_ids(row_adapter, rows: int, like):
+    if row_adapter is None:
+        return None
+    import torch
+    if row_adapter.shape != (rows,) or row_adapter.dtype != torch.int32 or row_adapter.device != like.device or not row_adapter.is_contiguous():
+        raise ValueError("row_adapter: expected a contiguous int32 tensor, one number per row")
+    return row_adapter.data_ptr()
+
+
+def _adapter_scratch(ad: CmoeAdapters, rows: int, ids, backward: int, scratch, like):
+    """The scratch of a call; allocated here where the caller gives none."""
+    import torch
+    if scratch is None:
+        nbytes = load().cmoe_adapter_scratch_bytes(C.byref(ad), rows, 0 if ids is None else 1, backward)
+        return torch.empty(nbytes, dtype=torch.uint8, device=like.device) if nbytes else None
+    if scratch.device != like.device or not scratch.is_contiguous() or scratch.dtype != torch.uint8:
+        raise ValueError("scratch: expected a contiguous uint8 tensor on the device of the rows")
+    return scratch
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def adapter_forward(x, a, b, row_adapter=None, scale=None, base=None, dropout: Optional[Dropout] = None, want_z: bool = False,
+                    out=None, z=None, scratch=None, stream=None):
+    """cmoe_adapter_forward on CUDA tensors: out[t] = base[t] + scale[i] * b[i] @ (a[i] @ x[t]) with i = row_adapter[t]
+    (outside [0, n): out[t] = base[t]; None: every row takes adapter 0).
+    x [rows, d_in], base / out [rows, d_out] (rows may be strided), a [n, rank, d_in], b [n, d_out, rank], row_adapter int32
+    [rows], scale float32 [n].  Returns out, or (out, z) with z float32 [rows, rank] for adapter_backward."""
+    import torch
+    rows, d_in = _rows(x, "x")
+    ad = _adapters(x, a, b, scale)
+    if d_in != ad.d_in:
+        raise ValueError(f"x: expected rows of {ad.d_in}")
+    if base is not None:
+        _matrix(base, "base", rows, ad.d_out, x)
+    if z is not None and (z.shape != (rows, ad.rank) or z.dtype != torch.float32 or z.device != x.device or not z.is_contiguous()):
+        raise ValueError("z: expected a contiguous float32 [rows, rank]")
+    ids, cfg = _adapter_ids(row_adapter, rows, x), _drop_config(dropout)
+    with _on(x, stream):
+        out = _out(out, "out", rows, ad.d_out, x)
+        if z is None and want_z:
+            z = torch.empty((rows, ad.rank), dtype=torch.float32, device=x.device)
+        scratch = _adapter_scratch(ad, rows, ids, 0, scratch, x)
+        st = load().cmoe_adapter_forward(C.byref(ad), x.data_ptr(), _ld(x), ids, rows, None if cfg is None else C.byref(cfg),
+                                         _ptr(base), 0 if base is None else _ld(base), out.data_ptr(), _ld(out), _ptr(z),
+                                         _ptr(scratch), 0 if scratch is None else scratch.numel(), _stream_ptr(None))
+    _check(st, "cmoe_adapter_forward")
+    return out if z is None else (out, z)
+
+
+def adapter_backward(dy, x, z, a, b, row_adapter=None, scale=None, dx_base=None, dropout: Optional[Dropout] = None,
+                     want_dx: bool = True, want_grads: bool = True, dx=None, grad_a=None, grad_b=None, scratch=None, stream=None):
+    """cmoe_adapter_backward on CUDA tensors: (dx, grad_a, grad_b) of adapter_forward's out for its gradient dy, with the
+    forward's x, z, row_adapter, scale and dropout; dx_base is added to dx.  Gradients that are not wanted are None."""
+    import torch
+    rows, d_out = _rows(dy, "dy")
+    ad = _adapters(dy, a, b, scale)
+    if d_out != ad.d_out:
+        raise ValueError(f"dy: expected rows of {ad.d_out}")
+    want_dx, want_grads = want_dx or dx is not None, want_grads or grad_a is not None or grad_b is not None
+    if want_grads:
+        _matrix(x, "x", rows, ad.d_in, dy)
+        if z.shape != (rows, ad.rank) or z.dtype != torch.float32 or z.device != dy.device or not z.is_contiguous():
+            raise ValueError("z: expected a contiguous float32 [rows, rank]")
+    if dx_base is not None:
+        _matrix(dx_base, "dx_base", rows, ad.d_in, dy)
+    for t, like in ((grad_a, a), (grad_b, b)):
+        if t is not None and (t.shape != like.shape or t.dtype != like.dtype or t.device != like.device or not t.is_contiguous()):
+            raise ValueError("grad_a / grad_b: expected contiguous tensors like a / b")
+    ids, cfg = _adapter_ids(row_adapter, rows, dy), _drop_config(dropout)
+    with _on(dy, stream):
+        if want_dx:
+            dx = _out(dx, "dx", rows, ad.d_in, dy)
+        if want_grads:
+            grad_a = torch.empty_like(a) if grad_a is None else grad_a
+            grad_b = torch.empty_like(b) if grad_b is None else grad_b
+        scratch = _adapter_scratch(ad, rows, ids, 1, scratch, dy)
+        st = load().cmoe_adapter_backward(C.byref(ad), dy.data_ptr(), _ld(dy), _ptr(x) if want_grads else None,
+                                          _ld(x) if want_grads else 0, _ptr(z) if want_grads else None, ids, rows,
+                                          None if cfg is None else C.byref(cfg), _ptr(dx_base),
+                                          0 if dx_base is None else _ld(dx_base), _ptr(dx), 0 if dx is None else _ld(dx),
+                                          _ptr(grad_a), _ptr(grad_b), _ptr(scratch), 0 if scratch is None else scratch.numel(),
+                                          _stream_ptr(None))
+    _check(st, "cmoe_adapter_backward")
+    return dx, grad_a, grad_b
+
+
+def adapter_scratch_bytes(n_adapters: int, rank: int, d_in: int, d_out: int, dtype, n_rows: int, with_row_adapter: bool = True,
+                          backward: bool = False) -> int:
+    """cmoe_adapter_scratch_bytes; dtype: torch.bfloat16 or torch.float32."""
+    import torch
+    code = {torch.bfloat16: CMOE_BF16, torch.float32: CMOE_FP32}[dtype]
+    ad = CmoeAdapters(n_adapters, rank, d_in, d_out, code, None, None, None)
+    return int(load().cmoe_adapter_scratch_bytes(C.byref(ad), n_rows, int(with_row_adapter), int(backward)))

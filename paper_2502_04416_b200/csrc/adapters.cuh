@@ -1,0 +1,1087 @@
+// Low-rank adapters of many requests beside a shared projection, and their gradients.
+//
+//   forward    z_t = A_a xd_t,  out_t = base_t + s_a B_a z_t             a: the adapter of row t, xd = x or its dropout
+//   backward   e_t = s_a B_a^T g_t,  dx_t = dx_base_t + m_t (A_a^T e_t),  dA_a = sum e_t xd_t^T,  dB_a = sum s_a g_t z_t^T
+//
+// Both directions are the same two products around a narrow middle (the rank, 8 to 64): rows [d_k] -> [r] -> [d_n], with
+// the weights of the second direction read in their other orientation.  One kernel does both products for a tile of rows
+// of one adapter and never writes the middle to global memory unless it is wanted; a second kernel forms the two
+// gradients of the weights, sums over the rows of an adapter.
+//
+// Bound: HBM (rows read once, outputs written once; 2 r flops an element).  At a rank of 64 that is 64 flops a byte, a
+// quarter of what the tensor cores could do at this bandwidth, so the products are warp-level MMAs on fragments that are
+// loaded straight from global memory, 16 bytes a lane: no staging through shared memory, and a lane's 16 bytes are the
+// eight elements that share one block of the dropout generator, so the mask costs no exchange either.
+#pragma once
+
+#include "common.cuh"
+#include "dropout.cuh"
+#include "permute.cuh"
+#include "router_cluster.cuh"
+#include "router_mma.cuh"
+
+namespace cmoe {
+
+constexpr int kAdMaxRank = 64;
+constexpr int kAdMaxAdapters = 1024;
+constexpr int kAdThreads = 256, kAdWarps = 8;
+constexpr int kAdSmallRows = 256;      // rows whose tiles every cluster finds for itself
+constexpr int kAdMaxRows = 1 << 30;
+
+// ---------------------------------------------------------------------------------------------------------------------
+// Tiles: up to M rows of one adapter.
+
+struct AdTiles {
+  const int32_t* row_adapter;    // null: every row takes adapter 0
+  int planned;                   // the lists below are there
+  const int32_t *tile_start;     // [n + 2] first tile of every adapter; group n: rows without an adapter
+  const int32_t *tile_adapter;   // [tiles]
+  const int32_t *row_list;       // [tiles * M] rows of the tiles, in order; -1 behind a group's last row
+};
+
+struct AdPlanOut { int32_t *tile_start, *tile_adapter, *row_list; };
+
+// The tiles of a batch, by one block: a stable counting sort of the rows by adapter (so sums over an adapter's rows have
+// a fixed order).  A warp owns a run of rows; lanes with the same adapter find each other by match, so no atomics.
+__global__ void __launch_bounds__(1024)
+adapter_plan_kernel(const int32_t* row_adapter, int n_rows, int n, int m, const AdPlanOut o) {
+  grid_dep_wait();
+  grid_dep_trigger();
+  extern __shared__ int32_t sm[];
+  const int groups = n + 1;
+  int32_t* hist = sm;                        // [32][groups]
+  int32_t* count = hist + 32 * groups;       // [groups]
+  int32_t* tiles = count + groups;           // [groups]
+  int32_t* start = tiles + groups;           // [groups + 1]
+  int32_t* sums = start + groups + 1;        // [32]
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const unsigned lt = (1u << lane) - 1u;
+  const long long per = (((long long)n_rows + 31) / 32 + 31) / 32 * 32;
+  const long long lo = warp * per, hi = min(lo + per, (long long)n_rows);
+  for (int i = threadIdx.x; i < 32 * groups; i += blockDim.x) hist[i] = 0;
+  __syncthreads();
+  int32_t* mine = hist + warp * groups;
+  auto group_of = [&](long long row) {
+    if (row >= hi) return -1;
+    const int v = __ldcg(row_adapter + row);
+    return (unsigned)v < (unsigned)n ? v : n;
+  };
+#pragma unroll 4
+  for (long long r0 = lo; r0 < hi; r0 += 32) {
+    const int g = group_of(r0 + lane);
+    const unsigned same = __match_any_sync(0xffffffffu, g);
+    if (g >= 0 && (same & lt) == 0) mine[g] += __popc(same);
+    __syncwarp();
+  }
+  __syncthreads();
+  for (int g = threadIdx.x; g < groups; g += blockDim.x) {
+    int run = 0;
+    for (int w = 0; w < 32; ++w) { const int v = hist[w * groups + g]; hist[w * groups + g] = run; run += v; }
+    count[g] = run;
+    tiles[g] = (run + m - 1) / m;
+  }
+  __syncthreads();
+  block_scan_groups(tiles, start, groups, sums);
+  for (int g = threadIdx.x; g <= groups; g += blockDim.x) o.tile_start[g] = start[g];
+  const int n_tiles = start[groups];
+  for (int t = threadIdx.x; t < n_tiles; t += blockDim.x) {
+    int a = 0, b = groups;                   // start[a] <= t < start[b]
+    while (b - a > 1) {
+      const int c = (a + b) >> 1;
+      if (start[c] <= t) a = c; else b = c;
+    }
+    o.tile_adapter[t] = a;
+    for (int i = max(0, count[a] - (t - start[a]) * m); i < m; ++i) o.row_list[(size_t)t * m + i] = -1;
+  }
+#pragma unroll 4
+  for (long long r0 = lo; r0 < hi; r0 += 32) {
+    const int g = group_of(r0 + lane);
+    const unsigned same = __match_any_sync(0xffffffffu, g);
+    const int before = g >= 0 ? mine[g] : 0;
+    __syncwarp();
+    if (g >= 0) {
+      o.row_list[(size_t)start[g] * m + before + __popc(same & lt)] = (int32_t)(r0 + lane);
+      if ((same & lt) == 0) mine[g] = before + __popc(same);
+    }
+    __syncwarp();
+  }
+}
+inline size_t adapter_plan_smem(int n) { return (size_t)(35 * (n + 1) + 1 + 32) * sizeof(int32_t); }
+
+// Rows of tile `tile` into rows[M] (-1: none); returns its adapter, n where its rows have none, or -1: nothing to do.
+// Every thread of the block calls it, and every block of a cluster gets the same answer.
+template <int M>
+__device__ __forceinline__ int adapter_tile(const AdTiles& t, int n_rows, int n, int tile, int32_t* rows) {
+  if (t.row_adapter == nullptr) {
+    for (int i = threadIdx.x; i < M; i += kAdThreads) {
+      const long long r = (long long)tile * M + i;
+      rows[i] = r < n_rows ? (int32_t)r : -1;
+    }
+    __syncthreads();
+    return 0;
+  }
+  if (t.planned) {
+    if (tile >= __ldcg(t.tile_start + n + 1)) return -1;
+    for (int i = threadIdx.x; i < M; i += kAdThreads) rows[i] = __ldcg(t.row_list + (size_t)tile * M + i);
+    __syncthreads();
+    return __ldcg(t.tile_adapter + tile);
+  }
+  // tile: the row that may head a tile.  It does if a multiple of M rows with its adapter come before it.
+  __shared__ uint32_t words[kAdSmallRows / 32];
+  __shared__ int32_t head;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  int a = -2;
+  if ((int)threadIdx.x < n_rows) {
+    a = __ldcg(t.row_adapter + threadIdx.x);
+    a = (unsigned)a < (unsigned)n ? a : n;
+  }
+  if ((int)threadIdx.x == tile) head = a;
+  for (int i = threadIdx.x; i < M; i += kAdThreads) rows[i] = -1;
+  __syncthreads();
+  const int mine = head;
+  const uint32_t vote = __ballot_sync(0xffffffffu, a == mine);
+  if (lane == 0) words[warp] = vote;
+  __syncthreads();
+  int rank = __popc(vote & ((1u << lane) - 1u)), first = 0;
+  for (int w = 0; w < kAdSmallRows / 32; ++w) {
+    if (w < warp) rank += __popc(words[w]);
+    if (w < (tile >> 5)) first += __popc(words[w]);
+  }
+  first += __popc(words[tile >> 5] & ((1u << (tile & 31)) - 1u));
+  if (first % M != 0) return -1;
+  if (a == mine && rank >= first && rank < first + M) rows[rank - first] = threadIdx.x;
+  __syncthreads();
+  return mine;
+}
+
+// ---------------------------------------------------------------------------------------------------------------------
+
+template <typename T> struct AdapterArgs {
+  const T* x; long long ldx;             // [rows, d_k]
+  const T *w1, *w2;                      // forward: A [n][r][d_k], B [n][d_n][r]; backward: B [n][d_k][r], A [n][r][d_n]
+  const float* scale;                    // [n] or null: 1
+  const T* base; long long ld_base;      // [rows, d_n] or null: 0
+  T* out; long long ld_out;              // [rows, d_n]; null: not wanted
+  float* z_out;                          // [rows, r] or null: the middle, unscaled (forward)
+  const float* z_in;                     // backward: the forward's z, for the operand of dB
+  void *u_e, *u_z;                       // backward: s e / (1 - p) and s z in the order of the tiles, or null
+  int n_rows, n, r, d_k, d_n;
+  AdTiles tiles;
+  Drop drop;
+};
+
+// A 32-bit float as two bf16 whose sum has at least 15 of its significant bits (the high part cut off, so that it never
+// rounds up to infinity; the low part zero where the value is not finite): the middle and the sums over rows lose
+// nothing that a bf16 result could show, for twice the MMAs of a narrow product.
+__device__ __forceinline__ void split_bf16(float v, uint16_t& hi, uint16_t& lo) {
+  const uint32_t u = __float_as_uint(v) & 0xffff0000u;
+  hi = (uint16_t)(u >> 16);
+  const float rest = (u & 0x7f800000u) == 0x7f800000u ? 0.0f : v - __uint_as_float(u);
+  lo = __bfloat16_as_ushort(__float2bfloat16_rn(rest));
+}
+// Transposes an 8 x 8 matrix of 16-bit elements held by the warp (lane 4 i + j: row i, columns 2 j and 2 j + 1).
+__device__ __forceinline__ uint32_t transpose8(uint32_t v) {
+  uint32_t r;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+  return r;
+}
+__device__ __forceinline__ void push4(uint32_t addr, float4 v) {
+  asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
+}
+__device__ __forceinline__ uint32_t cluster_ctas() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ uint32_t ld4(const void* p) {
+  uint32_t r;
+  asm volatile("ld.global.b32 %0, [%1];" : "=r"(r) : "l"(p));
+  return r;
+}
+__device__ __forceinline__ uint2 ld8(const void* p) {
+  uint2 r;
+  asm volatile("ld.global.v2.b32 {%0, %1}, [%2];" : "=r"(r.x), "=r"(r.y) : "l"(p));
+  return r;
+}
+
+// Rows without an adapter: base goes to out, z is zero.  The blocks of a cluster share the columns.
+template <typename T>
+__device__ __forceinline__ void adapter_none(const AdapterArgs<T>& p, const int32_t* rows, int m, uint32_t rank, uint32_t ctas) {
+  const int vecs = p.d_n / 8;
+  const bool copy = p.out && !(p.base == p.out && p.ld_base == p.ld_out);
+  for (int i = 0; i < m; ++i) {
+    const int row = rows[i];
+    if (row < 0) break;
+    if (copy)
+      for (int c = (int)rank * kAdThreads + threadIdx.x; c < vecs; c += kAdThreads * ctas) {
+        float v[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+        if (p.base) load8(p.base + (size_t)row * p.ld_base + 8 * c, v);
+        store8(p.out + (size_t)row * p.ld_out + 8 * c, v);
+      }
+    if (p.z_out && rank == 0 && (int)threadIdx.x < p.r) p.z_out[(size_t)row * p.r + threadIdx.x] = 0.0f;
+  }
+}
+
+// ---- bf16 -------------------------------------------------------------------------------------------------------------
+// MT: 16-row MMA tiles of a row tile; RT: 8-wide tiles of the rank (padded with zeros); TRANS: backward.
+// Shared memory: part (the sums of four warps), recv (those of every block of the cluster), the middle as two bf16.
+template <int MT, int RT> struct AdapterSmem {
+  static constexpr int kM = 16 * MT, kR = 8 * RT, kStride = kR + 8;
+  static constexpr int kPart = 4 * kM * kR * 4, kRecv = kM * kR * 4, kMid = 2 * kM * kStride * 2;
+  static constexpr int bytes(int ctas) { return kPart + ctas * kRecv + kMid + kM * 4; }
+};
+
+template <int MT, int RT, bool TRANS, bool DROP>
+__global__ void __launch_bounds__(kAdThreads, MT * RT <= 8 ? 2 : 1)
+adapter_kernel(const AdapterArgs<bf16> p) {
+  using S = AdapterSmem<MT, RT>;
+  constexpr int M = S::kM, kStride = S::kStride, kQuads = MT * RT * 32;
+  extern __shared__ __align__(16) uint8_t smem[];
+  const uint32_t ctas = cluster_ctas(), rank = cluster_rank();
+  float4* part = reinterpret_cast<float4*>(smem);                              // [4][MT][RT][lane]
+  float4* recv = part + 4 * kQuads;                                            // [ctas][MT][RT][lane]
+  uint16_t* mid = reinterpret_cast<uint16_t*>(recv + ctas * kQuads);           // [high, low][M][kStride]
+  int32_t* rows = reinterpret_cast<int32_t*>(mid + 2 * M * kStride);
+  rc_cluster_arrive();                                                         // this block has started
+  grid_dep_wait();
+  grid_dep_trigger();
+  const int tile = blockIdx.x / ctas;
+  const int a = adapter_tile<M>(p.tiles, p.n_rows, p.n, tile, rows);
+  if (a < 0 || a == p.n) {                                                     // the whole cluster leaves
+    if (a == p.n) adapter_none(p, rows, M, rank, ctas);
+    rc_cluster_wait();
+    return;
+  }
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
+  const int wi = (int)rank * kAdWarps + warp, nw = (int)ctas * kAdWarps;
+  const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+
+  // ---- first product: [M, d_k] x [d_k, r], 32-wide blocks of d_k dealt to the warps of the cluster
+  float acc[MT][RT][4];
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) acc[mt][rt][i] = 0.0f;
+  const bf16* xr[MT][2];
+  int row_of[MT][2];
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int row = rows[mt * 16 + 8 * h + g];
+      row_of[mt][h] = row < 0 ? rows[0] : row;           // a row's sums are its own: rows past the end repeat the first
+      xr[mt][h] = p.x + (size_t)row_of[mt][h] * p.ldx + 8 * q;
+    }
+  const bf16* w1 = p.w1 + (size_t)a * p.r * p.d_k;
+  const int kb_end = (p.d_k + 31) >> 5;
+  struct Step { uint4 x[MT][2]; uint32_t w[RT][4]; };
+  auto load_step = [&](int kb, Step& s) {
+    const bool in = kb * 32 + 8 * q < p.d_k;
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) s.x[mt][h] = in ? ld_dep16(xr[mt][h] + kb * 32) : zero;
+    if (!TRANS) {
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) {
+        const uint4 v = in && rt * 8 + g < p.r ? ld_dep16(w1 + (size_t)(rt * 8 + g) * p.d_k + kb * 32 + 8 * q) : zero;
+        s.w[rt][0] = v.x; s.w[rt][1] = v.y; s.w[rt][2] = v.z; s.w[rt][3] = v.w;
+      }
+    } else {
+      // rows of [d_k][r]: matrix i holds k = 8 (g / 2) + 2 i + g % 2, so that transposed it holds a lane's k = 8 q + 2 i, + 1
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int k = kb * 32 + 8 * (g >> 1) + 2 * i + (g & 1);
+        const bf16* wr = w1 + (size_t)k * p.r;
+        if (RT == 1) {
+          s.w[0][i] = k < p.d_k ? ld4(wr + 2 * q) : 0u;
+        } else if (RT == 2) {
+          const uint2 v = k < p.d_k ? ld8(wr + 4 * q) : make_uint2(0u, 0u);
+          s.w[0][i] = v.x; s.w[RT - 1][i] = v.y;
+        } else {
+#pragma unroll
+          for (int h = 0; h < RT / 4; ++h) {
+            const uint4 v = k < p.d_k && 32 * h + 8 * q < p.r ? ld_dep16(wr + 32 * h + 8 * q) : zero;
+            s.w[(4 * h) % RT][i] = v.x; s.w[(4 * h + 1) % RT][i] = v.y; s.w[(4 * h + 2) % RT][i] = v.z; s.w[(4 * h + 3) % RT][i] = v.w;
+          }
+        }
+      }
+    }
+  };
+  auto use_step = [&](int kb, Step& s) {
+    if (TRANS) {
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s.w[rt][i] = transpose8(s.w[rt][i]);
+    }
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+      if (DROP && !TRANS)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) s.x[mt][h] = drop8(s.x[mt][h], drop_draws(p.drop, row_of[mt][h], kb * 4 + q), p.drop.thr16);
+      const uint4 lo = s.x[mt][0], hi = s.x[mt][1];
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) {
+        mma_bf16_16816(acc[mt][rt], lo.x, hi.x, lo.y, hi.y, s.w[rt][0], s.w[rt][1]);
+        mma_bf16_16816(acc[mt][rt], lo.z, hi.z, lo.w, hi.w, s.w[rt][2], s.w[rt][3]);
+      }
+    }
+  };
+  {
+    Step cur, nxt;
+    if (wi < kb_end) load_step(wi, cur);
+#pragma unroll 1
+    for (int kb = wi; kb < kb_end; kb += nw) {
+      if (kb + nw < kb_end) load_step(kb + nw, nxt);
+      use_step(kb, cur);
+      cur = nxt;
+    }
+  }
+
+  // ---- second product's operands of this warp's first 32 columns: in flight while the sums meet
+  const bf16* w2 = p.w2 + (size_t)a * p.r * p.d_n;
+  const int nb_end = p.out ? (p.d_n + 31) >> 5 : 0;
+  struct Cols { uint32_t w[4][RT]; uint4 base[MT][2]; };
+  auto load_cols = [&](int nb, Cols& s) {
+    if (!TRANS) {
+      // tile j's column g stands for column 8 (g / 2) + 2 j + g % 2, so that a lane's results are columns 8 q .. 8 q + 7
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int c = nb * 32 + 8 * (g >> 1) + 2 * j + (g & 1);
+        const bf16* wr = w2 + (size_t)c * p.r;
+        if (RT == 1) {
+          s.w[j][0] = c < p.d_n ? ld4(wr + 2 * q) : 0u;
+        } else if (RT == 2) {
+          const uint2 v = c < p.d_n ? ld8(wr + 4 * q) : make_uint2(0u, 0u);
+          s.w[j][0] = v.x; s.w[j][RT - 1] = v.y;
+        } else {
+#pragma unroll
+          for (int h = 0; h < RT / 4; ++h) {
+            const uint4 v = c < p.d_n && 32 * h + 8 * q < p.r ? ld_dep16(wr + 32 * h + 8 * q) : zero;
+            s.w[j][(4 * h) % RT] = v.x; s.w[j][(4 * h + 1) % RT] = v.y; s.w[j][(4 * h + 2) % RT] = v.z; s.w[j][(4 * h + 3) % RT] = v.w;
+          }
+        }
+      }
+    } else {
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) {
+        const uint4 v = rt * 8 + g < p.r && nb * 32 + 8 * q < p.d_n ? ld_dep16(w2 + (size_t)(rt * 8 + g) * p.d_n + nb * 32 + 8 * q) : zero;
+        s.w[0][rt] = v.x; s.w[1][rt] = v.y; s.w[2][rt] = v.z; s.w[3][rt] = v.w;
+      }
+    }
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        s.base[mt][h] = p.base && nb * 32 + 8 * q < p.d_n ? ld_dep16(p.base + (size_t)row_of[mt][h] * p.ld_base + nb * 32 + 8 * q) : zero;
+  };
+  Cols cur;
+  if (wi < nb_end) load_cols(wi, cur);
+
+  // ---- the sums of eight warps, then of the cluster's blocks, each in a fixed order
+  if (warp >= 4)
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt)
+        part[(warp - 4) * kQuads + (mt * RT + rt) * 32 + lane] = make_float4(acc[mt][rt][0], acc[mt][rt][1], acc[mt][rt][2], acc[mt][rt][3]);
+  __syncthreads();
+  if (warp < 4)
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) {
+        float4& s = part[warp * kQuads + (mt * RT + rt) * 32 + lane];
+        s = make_float4(s.x + acc[mt][rt][0], s.y + acc[mt][rt][1], s.z + acc[mt][rt][2], s.w + acc[mt][rt][3]);
+      }
+  __syncthreads();
+  rc_cluster_wait();                                                           // every peer has started
+  for (int i = threadIdx.x; i < kQuads; i += kAdThreads) {
+    float4 s = part[i];
+#pragma unroll
+    for (int w = 1; w < 4; ++w) {
+      const float4 v = part[w * kQuads + i];
+      s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+    }
+    for (uint32_t c = 0; c < ctas; ++c) push4(rc_peer(recv + rank * kQuads + i, c), s);
+  }
+  rc_cluster_arrive();
+  rc_cluster_wait();
+  const float scale = p.scale ? __ldcg(p.scale + a) : 1.0f;
+  const float drop_inv = DROP ? p.drop.inv : 1.0f;
+  for (int i = threadIdx.x; i < kQuads; i += kAdThreads) {
+    float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    for (uint32_t c = 0; c < ctas; ++c) {
+      const float4 v = recv[c * kQuads + i];
+      s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+    }
+    const int l = i & 31, rt = (i >> 5) % RT, mt = (i >> 5) / RT, lg = l >> 2, lq = l & 3;
+    int n0 = rt * 8 + 2 * lq;                                                  // rank of the lane's first column
+    if (TRANS && RT == 2) n0 = 4 * lq + 2 * rt;
+    if (TRANS && RT >= 4) n0 = (rt >> 2) * 32 + 8 * lq + 2 * (rt & 3);
+    const float v[2][2] = {{s.x * drop_inv, s.y * drop_inv}, {s.z * drop_inv, s.w * drop_inv}};
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int m = mt * 16 + 8 * h + lg, row = rows[m];
+      if (p.z_out && row >= 0 && n0 < p.r && (uint32_t)(i >> 5) % ctas == rank)
+        *reinterpret_cast<float2*>(p.z_out + (size_t)row * p.r + n0) = make_float2(v[h][0], v[h][1]);
+      uint16_t hi[2], lo[2];
+#pragma unroll
+      for (int e = 0; e < 2; ++e) split_bf16(row >= 0 && n0 < p.r ? v[h][e] * scale : 0.0f, hi[e], lo[e]);
+      *reinterpret_cast<uint32_t*>(mid + m * kStride + n0) = hi[0] | (uint32_t)hi[1] << 16;
+      *reinterpret_cast<uint32_t*>(mid + (M + m) * kStride + n0) = lo[0] | (uint32_t)lo[1] << 16;
+    }
+  }
+  __syncthreads();
+
+  // ---- backward: the middle and the forward's as MMA fragments for the sums over rows (16 rows x 8 ranks a warp)
+  if (TRANS && p.u_e) {
+    uint4* ue = reinterpret_cast<uint4*>(p.u_e) + (size_t)tile * kQuads;
+    uint4* uz = reinterpret_cast<uint4*>(p.u_z) + (size_t)tile * kQuads;
+    for (int i = threadIdx.x; i < kQuads; i += kAdThreads) {
+      if ((uint32_t)(i >> 5) % ctas != rank) continue;
+      const int l = i & 31, rt = (i >> 5) % RT, mt = (i >> 5) / RT, nn = rt * 8 + (l >> 2), t0 = mt * 16 + 2 * (l & 3);
+      uint16_t eh[4], el[4], zh[4], zl[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int m = t0 + (j & 1) + 8 * (j >> 1), row = rows[m];
+        eh[j] = mid[m * kStride + nn];
+        el[j] = mid[(M + m) * kStride + nn];
+        split_bf16(row >= 0 && nn < p.r ? __ldcg(p.z_in + (size_t)row * p.r + nn) * scale : 0.0f, zh[j], zl[j]);
+      }
+      ue[i] = make_uint4(eh[0] | (uint32_t)eh[1] << 16, eh[2] | (uint32_t)eh[3] << 16, el[0] | (uint32_t)el[1] << 16, el[2] | (uint32_t)el[3] << 16);
+      uz[i] = make_uint4(zh[0] | (uint32_t)zh[1] << 16, zh[2] | (uint32_t)zh[3] << 16, zl[0] | (uint32_t)zl[1] << 16, zl[2] | (uint32_t)zl[3] << 16);
+    }
+  }
+
+  // ---- second product: [M, r] x [r, d_n], added to base
+  auto ld_mid4 = [&](int part_, int m, int c) { return *reinterpret_cast<const uint32_t*>(mid + (part_ * M + m) * kStride + c); };
+#pragma unroll 1
+  for (int nb = wi; nb < nb_end; nb += nw) {
+    Cols nxt;
+    if (nb + nw < nb_end) load_cols(nb + nw, nxt);
+    if (TRANS) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) cur.w[j][rt] = transpose8(cur.w[j][rt]);
+    }
+    const int c = nb * 32 + 8 * q;
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+      float o[4][4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[j][i] = 0.0f;
+      const int m0 = mt * 16 + g, m1 = m0 + 8;
+      if (RT == 1) {                               // one MMA: k 0 .. 7 the high part, 8 .. 15 the low part
+        const uint32_t a0 = ld_mid4(0, m0, 2 * q), a1 = ld_mid4(0, m1, 2 * q), a2 = ld_mid4(1, m0, 2 * q), a3 = ld_mid4(1, m1, 2 * q);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) mma_bf16_16816(o[j], a0, a1, a2, a3, cur.w[j][0], cur.w[j][0]);
+      } else {
+#pragma unroll
+        for (int s = 0; s < RT / 2; ++s) {
+          // k of step s: ranks 16 s .. 16 s + 15 as they lie (TRANS), else a lane's own four neighbours
+          const int c0 = TRANS ? 16 * s + 2 * q : RT == 2 ? 4 * q : (s >> 1) * 32 + 8 * q + 4 * (s & 1);
+          const int c1 = TRANS ? c0 + 8 : c0 + 2;
+#pragma unroll
+          for (int lo = 1; lo >= 0; --lo) {
+            const uint32_t a0 = ld_mid4(lo, m0, c0), a1 = ld_mid4(lo, m1, c0), a2 = ld_mid4(lo, m0, c1), a3 = ld_mid4(lo, m1, c1);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) mma_bf16_16816(o[j], a0, a1, a2, a3, cur.w[j][(2 * s) % RT], cur.w[j][(2 * s + 1) % RT]);
+          }
+        }
+      }
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int row = rows[mt * 16 + 8 * h + g];
+        if (row < 0 || c >= p.d_n) continue;
+        float v[8];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) { v[2 * j] = o[j][2 * h]; v[2 * j + 1] = o[j][2 * h + 1]; }
+        if (DROP && TRANS) drop8(v, drop_draws(p.drop, row, c >> 3), p.drop.thr16);
+        const uint32_t b[4] = {cur.base[mt][h].x, cur.base[mt][h].y, cur.base[mt][h].z, cur.base[mt][h].w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          v[2 * j] += __uint_as_float(b[j] << 16);
+          v[2 * j + 1] += __uint_as_float(b[j] & 0xffff0000u);
+        }
+        store8(p.out + (size_t)row * p.ld_out + c, v);
+      }
+    }
+    cur = nxt;
+  }
+}
+
+// ---- the gradients of the weights, bf16 ---------------------------------------------------------------------------------
+// G[c][k] = sum over the adapter's rows t of V[t][c] U[t][k]: V = x under its mask with U = s e / (1 - p) for dA, V = g with
+// U = s z for dB.  A block owns kOutCols columns; its warps split the columns four ways and the rows two ways, the
+// blocks of a cluster split the rows further and add their sums through each other's shared memory, in rank order.
+constexpr int kOutColWarps = 4, kOutCols = 64 * kOutColWarps, kOutRowWarps = kAdWarps / kOutColWarps;
+
+struct OuterSide {
+  const void* v; long long ldv;
+  const void* u;
+  void* g;
+  int d;
+};
+struct OuterArgs {
+  OuterSide side[2];           // 0: dA [n][r][d], 1: dB [n][d][r]
+  int slices0;                 // column slices of side 0
+  int n_rows, n, r, m;         // m: rows of a tile
+  AdTiles tiles;
+  Drop drop;
+};
+
+template <int RT> constexpr int kOutQuads = kOutColWarps * 4 * RT * 32;
+
+template <int RT, bool DROP>
+__global__ void __launch_bounds__(kAdThreads, RT <= 4 ? 2 : 1)
+adapter_outer_kernel(const OuterArgs p) {
+  constexpr int kQuads = kOutQuads<RT>;
+  extern __shared__ __align__(16) uint8_t smem[];
+  float4* part = reinterpret_cast<float4*>(smem);          // the second half of the rows
+  float4* recv = part + kQuads;                            // [ctas][kQuads / ctas]
+  const uint32_t ctas = cluster_ctas(), rank = cluster_rank();
+  rc_cluster_arrive();
+  grid_dep_wait();
+  grid_dep_trigger();
+  const int side = (int)blockIdx.x < p.slices0 ? 0 : 1, slice = blockIdx.x - (side ? p.slices0 : 0), a = blockIdx.y;
+  const OuterSide sd = p.side[side];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
+  const int cw = warp % kOutColWarps, rw = warp / kOutColWarps;
+  int t_lo = 0, t_hi = (p.n_rows + 15) / 16;               // 16-row tiles
+  if (p.tiles.row_adapter) {
+    t_lo = __ldcg(p.tiles.tile_start + a) * (p.m / 16);
+    t_hi = __ldcg(p.tiles.tile_start + a + 1) * (p.m / 16);
+  } else if (a > 0) {
+    t_hi = 0;
+  }
+  const int c0 = slice * kOutCols + cw * 64;
+  const bf16* v = (const bf16*)sd.v;
+  const uint4* u = (const uint4*)sd.u;
+  const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+  const bool drop = DROP && side == 0;
+  float acc[4][RT][4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[i][rt][e] = 0.0f;
+  const int step = (int)ctas * kOutRowWarps;
+  if (c0 < sd.d) {
+#pragma unroll 1
+    for (int t = t_lo + (int)rank * kOutRowWarps + rw; t < t_hi; t += step) {
+      uint4 x[2][2];                                       // [rows g, g + 8][columns 8 q .., 32 + 8 q ..]
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const long long pos = (long long)t * 16 + 8 * h + g;
+        const int row = p.tiles.row_adapter ? __ldcg(p.tiles.row_list + pos) : pos < p.n_rows ? (int)pos : -1;
+#pragma unroll
+        for (int w = 0; w < 2; ++w) {
+          const int c = c0 + 32 * w + 8 * q;
+          x[h][w] = row >= 0 && c < sd.d ? ld_dep16(v + (size_t)row * sd.ldv + c) : zero;
+          if (drop) x[h][w] = drop8(x[h][w], drop_draws(p.drop, row, c >> 3), p.drop.thr16);
+        }
+      }
+      uint4 uf[RT];
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) uf[rt] = ld_dep16(u + ((size_t)t * RT + rt) * 32 + lane);
+      // columns become the MMA's rows: tile (w, j / 2) has columns 32 w + 8 (i / 2) + 2 j + i % 2 of its rows i
+#pragma unroll
+      for (int w = 0; w < 2; ++w)
+#pragma unroll
+        for (int jp = 0; jp < 2; ++jp) {
+          const uint32_t l0 = jp ? x[0][w].z : x[0][w].x, l1 = jp ? x[0][w].w : x[0][w].y;
+          const uint32_t h0 = jp ? x[1][w].z : x[1][w].x, h1 = jp ? x[1][w].w : x[1][w].y;
+          const uint32_t a0 = transpose8(l0), a1 = transpose8(l1), a2 = transpose8(h0), a3 = transpose8(h1);
+#pragma unroll
+          for (int rt = 0; rt < RT; ++rt) {
+            mma_bf16_16816(acc[2 * w + jp][rt], a0, a1, a2, a3, uf[rt].z, uf[rt].w);
+            mma_bf16_16816(acc[2 * w + jp][rt], a0, a1, a2, a3, uf[rt].x, uf[rt].y);
+          }
+        }
+    }
+  }
+  auto quad = [&](int i, int rt) { return ((cw * 4 + i) * RT + rt) * 32 + lane; };
+  if (rw == 1)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) part[quad(i, rt)] = make_float4(acc[i][rt][0], acc[i][rt][1], acc[i][rt][2], acc[i][rt][3]);
+  __syncthreads();
+  rc_cluster_wait();
+  const int own = kQuads / (int)ctas;                      // quads that a block finishes
+  if (rw == 0)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) {
+        const int k = quad(i, rt);
+        const float4 s = part[k];
+        push4(rc_peer(recv + (int)rank * own + k % own, k / own),
+              make_float4(s.x + acc[i][rt][0], s.y + acc[i][rt][1], s.z + acc[i][rt][2], s.w + acc[i][rt][3]));
+      }
+  rc_cluster_arrive();
+  rc_cluster_wait();
+  bf16* out = (bf16*)sd.g + (size_t)a * p.r * sd.d;
+  for (int i = threadIdx.x; i < own; i += kAdThreads) {
+    float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    for (uint32_t c = 0; c < ctas; ++c) {
+      const float4 w = recv[c * own + i];
+      s.x += w.x; s.y += w.y; s.z += w.z; s.w += w.w;
+    }
+    const int k = (int)rank * own + i, l = k & 31, rt = (k >> 5) % RT, mi = (k >> 5) / RT;   // mi: column warp, tile
+    const int n0 = rt * 8 + 2 * (l & 3), lg = l >> 2;
+    if (n0 >= p.r) continue;
+    const float val[2][2] = {{s.x, s.y}, {s.z, s.w}};
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int c = slice * kOutCols + (mi >> 2) * 64 + ((mi >> 1) & 1) * 32 + 8 * (lg >> 1) + 2 * (2 * (mi & 1) + h) + (lg & 1);
+      if (c >= sd.d) continue;
+      if (side == 0) {
+        out[(size_t)n0 * sd.d + c] = __float2bfloat16_rn(val[h][0]);
+        out[(size_t)(n0 + 1) * sd.d + c] = __float2bfloat16_rn(val[h][1]);
+      } else {
+        *reinterpret_cast<uint32_t*>(out + (size_t)c * p.r + n0) = pack_bf16x2(val[h][0], val[h][1]);
+      }
+    }
+  }
+}
+
+// ---- fp32 -------------------------------------------------------------------------------------------------------------
+// The same tiles and exchange on the CUDA cores, with fused multiply-adds in full 32 bits.  A lane holds rows g, g + 8, ..
+// of the tile and eight neighbouring k (first product) or columns (second product); ranks go by in chunks of 16.
+constexpr int kSimtM = 32, kSimtRc = 16;
+struct AdapterSimtSmem {
+  static constexpr int kStride = kAdMaxRank + 4;
+  static constexpr int bytes(int ctas) {
+    return (kAdWarps * kSimtM * kSimtRc + kSimtM * kAdMaxRank + ctas * kSimtM * kAdMaxRank + kSimtM * kStride) * 4 + kSimtM * 4;
+  }
+};
+
+template <bool TRANS, bool DROP>
+__global__ void __launch_bounds__(kAdThreads, 2)
+adapter_simt_kernel(const AdapterArgs<float> p) {
+  constexpr int M = kSimtM, kStride = AdapterSimtSmem::kStride;
+  extern __shared__ __align__(16) uint8_t smem[];
+  const uint32_t ctas = cluster_ctas(), rank = cluster_rank();
+  float* part = reinterpret_cast<float*>(smem);                      // [warp][M][kSimtRc]
+  float* zpart = part + kAdWarps * M * kSimtRc;                      // [M][kAdMaxRank]
+  float* recv = zpart + M * kAdMaxRank;                              // [ctas][M][kAdMaxRank]
+  float* mid = recv + ctas * M * kAdMaxRank;                         // [M][kStride]
+  int32_t* rows = reinterpret_cast<int32_t*>(mid + M * kStride);
+  rc_cluster_arrive();
+  grid_dep_wait();
+  grid_dep_trigger();
+  const int tile = blockIdx.x / ctas;
+  const int a = adapter_tile<M>(p.tiles, p.n_rows, p.n, tile, rows);
+  if (a < 0 || a == p.n) {
+    if (a == p.n) adapter_none(p, rows, M, rank, ctas);
+    rc_cluster_wait();
+    return;
+  }
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
+  const int wi = (int)rank * kAdWarps + warp, nw = (int)ctas * kAdWarps;
+  int row_of[4];
+#pragma unroll
+  for (int m = 0; m < 4; ++m) row_of[m] = rows[8 * m + g] < 0 ? rows[0] : rows[8 * m + g];
+  const float* w1 = p.w1 + (size_t)a * p.r * p.d_k;
+  const int kb_end = (p.d_k + 31) >> 5;
+#pragma unroll 1
+  for (int rc = 0; rc < p.r; rc += kSimtRc) {
+    float acc[4][kSimtRc];
+#pragma unroll
+    for (int m = 0; m < 4; ++m)
+#pragma unroll
+      for (int j = 0; j < kSimtRc; ++j) acc[m][j] = 0.0f;
+#pragma unroll 1
+    for (int kb = wi; kb < kb_end; kb += nw) {
+      const int k = kb * 32 + 8 * q;
+      if (k < p.d_k) {                                               // d_k is a multiple of 8
+        float x[4][8];
+#pragma unroll
+        for (int m = 0; m < 4; ++m) {
+          load8(p.x + (size_t)row_of[m] * p.ldx + k, x[m]);
+          if (DROP && !TRANS) drop8(x[m], drop_draws(p.drop, row_of[m], k >> 3), p.drop.thr16);
+        }
+        if (!TRANS) {
+#pragma unroll
+          for (int j = 0; j < kSimtRc; ++j)
+            if (rc + j < p.r) {
+              float w[8];
+              load8(w1 + (size_t)(rc + j) * p.d_k + k, w);
+#pragma unroll
+              for (int m = 0; m < 4; ++m)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) acc[m][j] = fmaf(x[m][i], w[i], acc[m][j]);
+            }
+        } else {
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int h = 0; h < kSimtRc / 8; ++h)
+              if (rc + 8 * h < p.r) {
+                float w[8];
+                load8(w1 + (size_t)(k + i) * p.r + rc + 8 * h, w);
+#pragma unroll
+                for (int m = 0; m < 4; ++m)
+#pragma unroll
+                  for (int j = 0; j < 8; ++j) acc[m][8 * h + j] = fmaf(x[m][i], w[j], acc[m][8 * h + j]);
+              }
+        }
+      }
+    }
+#pragma unroll
+    for (int m = 0; m < 4; ++m)
+#pragma unroll
+      for (int j = 0; j < kSimtRc; ++j) {
+        float s = acc[m][j];
+        s += __shfl_xor_sync(0xffffffffu, s, 1);
+        s += __shfl_xor_sync(0xffffffffu, s, 2);
+        if ((j >> 2) == q) part[(warp * M + 8 * m + g) * kSimtRc + j] = s;
+      }
+    __syncthreads();
+    for (int i = threadIdx.x; i < M * kSimtRc; i += kAdThreads) {
+      float s = 0.0f;
+#pragma unroll
+      for (int w = 0; w < kAdWarps; ++w) s += part[w * M * kSimtRc + i];
+      zpart[(i / kSimtRc) * kAdMaxRank + rc + i % kSimtRc] = s;
+    }
+    __syncthreads();
+  }
+  rc_cluster_wait();
+  for (int i = threadIdx.x; i < M * (p.r / 4); i += kAdThreads) {
+    const int m = i / (p.r / 4), c = 4 * (i % (p.r / 4));
+    const float4 v = *reinterpret_cast<const float4*>(zpart + m * kAdMaxRank + c);
+    for (uint32_t k = 0; k < ctas; ++k) push4(rc_peer(recv + (rank * M + m) * kAdMaxRank + c, k), v);
+  }
+  rc_cluster_arrive();
+  rc_cluster_wait();
+  const float scale = p.scale ? __ldcg(p.scale + a) : 1.0f;
+  const float drop_inv = DROP ? p.drop.inv : 1.0f;
+  for (int i = threadIdx.x; i < M * p.r; i += kAdThreads) {
+    const int m = i / p.r, c = i - m * p.r, row = rows[m];
+    float s = 0.0f;
+    for (uint32_t k = 0; k < ctas; ++k) s += recv[(k * M + m) * kAdMaxRank + c];
+    s *= drop_inv;
+    const bool mine = (uint32_t)m % ctas == rank;
+    if (p.z_out && row >= 0 && mine) p.z_out[(size_t)row * p.r + c] = s;
+    s = row >= 0 ? s * scale : 0.0f;
+    mid[m * kStride + c] = s;
+    if (TRANS && p.u_e && mine) {
+      const size_t at = ((size_t)tile * M + m) * p.r + c;
+      reinterpret_cast<float*>(p.u_e)[at] = s;
+      reinterpret_cast<float*>(p.u_z)[at] = row >= 0 ? __ldcg(p.z_in + (size_t)row * p.r + c) * scale : 0.0f;
+    }
+  }
+  __syncthreads();
+  const float* w2 = p.w2 + (size_t)a * p.r * p.d_n;
+  const int nb_end = p.out ? (p.d_n + 31) >> 5 : 0;
+#pragma unroll 1
+  for (int nb = wi; nb < nb_end; nb += nw) {
+    const int c = nb * 32 + 8 * q;
+    if (c >= p.d_n) continue;
+    float o[4][8];
+#pragma unroll
+    for (int m = 0; m < 4; ++m)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) o[m][j] = 0.0f;
+#pragma unroll 1
+    for (int k = 0; k < p.r; k += 4) {
+      float4 z[4];
+#pragma unroll
+      for (int m = 0; m < 4; ++m) z[m] = *reinterpret_cast<const float4*>(mid + (8 * m + g) * kStride + k);
+      if (!TRANS) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const uint4 w = ld_dep16(w2 + (size_t)(c + j) * p.r + k);
+#pragma unroll
+          for (int m = 0; m < 4; ++m) {
+            o[m][j] = fmaf(z[m].x, __uint_as_float(w.x), o[m][j]);
+            o[m][j] = fmaf(z[m].y, __uint_as_float(w.y), o[m][j]);
+            o[m][j] = fmaf(z[m].z, __uint_as_float(w.z), o[m][j]);
+            o[m][j] = fmaf(z[m].w, __uint_as_float(w.w), o[m][j]);
+          }
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float w[8];
+          load8(w2 + (size_t)(k + i) * p.d_n + c, w);
+#pragma unroll
+          for (int m = 0; m < 4; ++m) {
+            const float zz = i == 0 ? z[m].x : i == 1 ? z[m].y : i == 2 ? z[m].z : z[m].w;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) o[m][j] = fmaf(zz, w[j], o[m][j]);
+          }
+        }
+      }
+    }
+#pragma unroll
+    for (int m = 0; m < 4; ++m) {
+      const int row = rows[8 * m + g];
+      if (row < 0) continue;
+      if (DROP && TRANS) drop8(o[m], drop_draws(p.drop, row, c >> 3), p.drop.thr16);
+      if (p.base) {
+        float b[8];
+        load8(p.base + (size_t)row * p.ld_base + c, b);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) o[m][j] += b[j];
+      }
+      store8(p.out + (size_t)row * p.ld_out + c, o[m]);
+    }
+  }
+}
+
+// Gradients of the weights in fp32: a block owns 64 columns and 16 ranks (two columns a lane), its warps and the blocks
+// of its cluster split the rows.  The masks of four rows come from one generator block a lane, by shuffles.
+constexpr int kSimtOutCols = 64;
+
+template <bool DROP>
+__global__ void __launch_bounds__(kAdThreads, 2)
+adapter_outer_simt_kernel(const OuterArgs p) {
+  __shared__ __align__(16) float part[kAdWarps][kSimtRc][kSimtOutCols];
+  __shared__ __align__(16) float recv[kSimtRc * kSimtOutCols];       // [ctas][kSimtRc * kSimtOutCols / ctas]
+  const uint32_t ctas = cluster_ctas(), rank = cluster_rank();
+  rc_cluster_arrive();
+  grid_dep_wait();
+  grid_dep_trigger();
+  const int chunks = (p.r + kSimtRc - 1) / kSimtRc;
+  const int side = (int)blockIdx.x < p.slices0 ? 0 : 1, slice = blockIdx.x - (side ? p.slices0 : 0);
+  const int a = blockIdx.y / chunks, rc = (blockIdx.y % chunks) * kSimtRc;
+  const OuterSide sd = p.side[side];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  int lo = 0, hi = p.n_rows;                                         // positions in the order of the tiles
+  if (p.tiles.row_adapter) {
+    lo = __ldcg(p.tiles.tile_start + a) * p.m;
+    hi = __ldcg(p.tiles.tile_start + a + 1) * p.m;
+  } else if (a > 0) {
+    hi = 0;
+  }
+  const float* v = (const float*)sd.v;
+  const float* u = (const float*)sd.u;
+  const int c = slice * kSimtOutCols + 2 * lane;
+  const bool in = c < sd.d, drop = DROP && side == 0;
+  float acc[2][kSimtRc];
+#pragma unroll
+  for (int j = 0; j < kSimtRc; ++j) acc[0][j] = acc[1][j] = 0.0f;
+  const int stride = (int)ctas * kAdWarps * 4;
+#pragma unroll 1
+  for (int t = lo + ((int)rank * kAdWarps + warp) * 4; t < hi; t += stride) {
+    int row[4];
+    uint2 x[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      row[i] = t + i < hi ? (p.tiles.row_adapter ? __ldcg(p.tiles.row_list + t + i) : t + i) : -1;
+      x[i] = row[i] >= 0 && in ? ld8(v + (size_t)row[i] * sd.ldv + c) : make_uint2(0u, 0u);
+    }
+    uint32_t bits = 0;
+    if (drop) {
+      const int mine = (lane >> 3) == 0 ? row[0] : (lane >> 3) == 1 ? row[1] : (lane >> 3) == 2 ? row[2] : row[3];
+      bits = keep_bits(drop_draws(p.drop, mine, (slice * kSimtOutCols >> 3) + (lane & 7)), p.drop.thr16);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (drop) {
+        const uint32_t b = __shfl_sync(0xffffffffu, bits, 8 * i + (lane >> 2)) >> (2 * (lane & 3));
+        if (!(b & 1u)) x[i].x = 0u;
+        if (!(b & 2u)) x[i].y = 0u;
+      }
+      if (row[i] < 0) continue;
+      const float x0 = __uint_as_float(x[i].x), x1 = __uint_as_float(x[i].y);
+#pragma unroll
+      for (int h = 0; h < kSimtRc / 8; ++h)
+        if (rc + 8 * h < p.r) {
+          float w[8];
+          load8(u + (size_t)(t + i) * p.r + rc + 8 * h, w);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            acc[0][8 * h + j] = fmaf(x0, w[j], acc[0][8 * h + j]);
+            acc[1][8 * h + j] = fmaf(x1, w[j], acc[1][8 * h + j]);
+          }
+        }
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < kSimtRc; ++j) *reinterpret_cast<float2*>(&part[warp][j][2 * lane]) = make_float2(acc[0][j], acc[1][j]);
+  __syncthreads();
+  rc_cluster_wait();
+  constexpr int kAll = kSimtRc * kSimtOutCols;
+  const int own = kAll / (int)ctas;
+  const float* flat = &part[0][0][0];
+  for (int i = 4 * threadIdx.x; i < kAll; i += 4 * kAdThreads) {
+    float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+    for (int w = 0; w < kAdWarps; ++w) {
+      const float4 f = *reinterpret_cast<const float4*>(flat + w * kAll + i);
+      s.x += f.x; s.y += f.y; s.z += f.z; s.w += f.w;
+    }
+    push4(rc_peer(recv + (int)rank * own + i % own, i / own), s);
+  }
+  rc_cluster_arrive();
+  rc_cluster_wait();
+  float* out = (float*)sd.g + (size_t)a * p.r * sd.d;
+  for (int i = threadIdx.x; i < own; i += kAdThreads) {
+    float s = 0.0f;
+    for (uint32_t k = 0; k < ctas; ++k) s += recv[k * own + i];
+    const int at = (int)rank * own + i, j = rc + at / kSimtOutCols, col = slice * kSimtOutCols + at % kSimtOutCols;
+    if (j < p.r && col < sd.d) out[side == 0 ? (size_t)j * sd.d + col : (size_t)col * p.r + j] = s;
+  }
+}
+
+// ---- host -------------------------------------------------------------------------------------------------------------
+
+inline int adapter_rank_tiles(int r) { return r <= 8 ? 1 : r <= 16 ? 2 : r <= 32 ? 4 : 8; }
+
+// 16-row MMA tiles of a row tile.  Batches whose clusters find their tiles themselves take 16 rows: most of their
+// adapters have a row or two.
+inline int adapter_mt(int r, bool small) { return small ? 1 : adapter_rank_tiles(r) == 8 ? 2 : 4; }
+inline bool adapter_small(const int32_t* row_adapter, int n_rows, bool backward) { return row_adapter && n_rows <= kAdSmallRows && !backward; }
+inline int adapter_tile_rows(bool bf, int r, bool small) { return bf ? 16 * adapter_mt(r, small) : kSimtM; }
+inline long long adapter_max_tiles(long long n_rows, int n, int m, bool one) {
+  return one ? (n_rows + m - 1) / m : n_rows / m + std::min<long long>(n + 1, n_rows);
+}
+
+struct AdapterScratch { size_t tile_start, tile_adapter, row_list, u_e, u_z, total; };
+inline AdapterScratch adapter_scratch(bool bf, int n_rows, int n, int r, bool backward, bool one) {
+  AdapterScratch s{};
+  const int m = adapter_tile_rows(bf, r, false);
+  const size_t tiles = (size_t)adapter_max_tiles(n_rows, n, m, one);
+  size_t at = 0;
+  const auto take = [&](size_t bytes) { const size_t p = at; at += (bytes + 255) / 256 * 256; return p; };
+  if (!one) {
+    s.tile_start = take((size_t)(n + 2) * 4);
+    s.tile_adapter = take(tiles * 4);
+    s.row_list = take(tiles * m * 4);
+  }
+  if (backward) {
+    const size_t u = tiles * m * (bf ? (size_t)adapter_rank_tiles(r) * 32 : (size_t)r * 4);
+    s.u_e = take(u);
+    s.u_z = take(u);
+  }
+  s.total = at;
+  return s;
+}
+
+constexpr size_t kAdPlainSmem = 46 * 1024;    // dynamic shared memory that needs no attribute next to the kernels' static variables
+
+// Blocks of a cluster for `tiles` tiles that have rows: enough for two rounds of the SMs, no more than have a 32-wide block of either product for each warp,
+// and no more than shared memory for their sums allows.
+inline int adapter_ctas(long long tiles, int n_sms, int widest, int smem_limit_ctas) {
+  int c = 1;
+  while (c < 8 && tiles * c < 2 * n_sms && c * 2 * kAdWarps <= std::max(kAdWarps, (widest + 31) / 32) && c * 2 <= smem_limit_ctas) c *= 2;
+  return c;
+}
+
+template <typename... KP, typename... A>
+inline cudaError_t launch_cluster(bool dep, void (*kernel)(KP...), dim3 grid, dim3 cluster, size_t smem, cudaStream_t st, A&&... args) {
+  if (smem > kAdPlainSmem) {
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e != cudaSuccess) return e;
+  }
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid; cfg.blockDim = dim3(kAdThreads); cfg.dynamicSmemBytes = smem; cfg.stream = st;
+  cudaLaunchAttribute at[2];
+  unsigned n = 0;
+  at[n].id = cudaLaunchAttributeClusterDimension;
+  at[n].val.clusterDim.x = cluster.x; at[n].val.clusterDim.y = cluster.y; at[n].val.clusterDim.z = cluster.z;
+  ++n;
+  if (dep) {
+    at[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[n++].val.programmaticStreamSerializationAllowed = 1;
+  }
+  cfg.attrs = at; cfg.numAttrs = n;
+  return cudaLaunchKernelEx(&cfg, kernel, std::forward<A>(args)...);
+}
+
+template <int MT, int RT, bool TRANS>
+inline cudaError_t launch_adapter_tile(const AdapterArgs<bf16>& a, long long tiles, long long live, int n_sms, bool dep, cudaStream_t st) {
+  const int room = std::max(1, (128 * 1024 - AdapterSmem<MT, RT>::bytes(0)) / AdapterSmem<MT, RT>::kRecv);
+  const int ctas = adapter_ctas(live, n_sms, std::max(a.d_k, a.d_n), room);
+  const size_t smem = AdapterSmem<MT, RT>::bytes(ctas);
+  const dim3 grid((unsigned)(tiles * ctas)), cl(ctas);
+  return a.drop.thr16 ? launch_cluster(dep, adapter_kernel<MT, RT, TRANS, true>, grid, cl, smem, st, a)
+                      : launch_cluster(dep, adapter_kernel<MT, RT, TRANS, false>, grid, cl, smem, st, a);
+}
+
+template <bool TRANS>
+inline cudaError_t launch_adapter(const AdapterArgs<bf16>& a, bool small, long long tiles, long long live, int n_sms, bool dep, cudaStream_t st) {
+  const int rt = adapter_rank_tiles(a.r);
+  if constexpr (!TRANS) {
+    if (small) switch (rt) {
+        case 1: return launch_adapter_tile<1, 1, TRANS>(a, tiles, live, n_sms, dep, st);
+        case 2: return launch_adapter_tile<1, 2, TRANS>(a, tiles, live, n_sms, dep, st);
+        case 4: return launch_adapter_tile<1, 4, TRANS>(a, tiles, live, n_sms, dep, st);
+        default: return launch_adapter_tile<1, 8, TRANS>(a, tiles, live, n_sms, dep, st);
+      }
+  }
+  switch (rt) {
+    case 1: return launch_adapter_tile<4, 1, TRANS>(a, tiles, live, n_sms, dep, st);
+    case 2: return launch_adapter_tile<4, 2, TRANS>(a, tiles, live, n_sms, dep, st);
+    case 4: return launch_adapter_tile<4, 4, TRANS>(a, tiles, live, n_sms, dep, st);
+    default: return launch_adapter_tile<2, 8, TRANS>(a, tiles, live, n_sms, dep, st);
+  }
+}
+template <bool TRANS>
+inline cudaError_t launch_adapter(const AdapterArgs<float>& a, bool, long long tiles, long long live, int n_sms, bool dep, cudaStream_t st) {
+  const int ctas = adapter_ctas(live, n_sms, std::max(a.d_k, a.d_n), 8);
+  const size_t smem = AdapterSimtSmem::bytes(ctas);
+  const dim3 grid((unsigned)(tiles * ctas)), cl(ctas);
+  return a.drop.thr16 ? launch_cluster(dep, adapter_simt_kernel<TRANS, true>, grid, cl, smem, st, a)
+                      : launch_cluster(dep, adapter_simt_kernel<TRANS, false>, grid, cl, smem, st, a);
+}
+
+template <typename T>
+inline cudaError_t launch_adapter_plan(const AdapterArgs<T>& a, int m, const AdPlanOut& o, cudaStream_t st) {
+  const size_t smem = adapter_plan_smem(a.n);
+  if (smem > kAdPlainSmem) {
+    const cudaError_t e = cudaFuncSetAttribute(adapter_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e != cudaSuccess) return e;
+  }
+  return launch_kernel(false, adapter_plan_kernel, dim3(1), dim3(1024), smem, st, a.tiles.row_adapter, a.n_rows, a.n, m, o);
+}
+
+// Blocks that share an adapter's rows: enough for two rounds of the SMs, and at least four steps for every warp.
+inline int outer_ctas(long long blocks, int n_sms, long long steps) {
+  int c = 1;
+  while (c < 8 && blocks * c < 2 * n_sms && steps >= 8 * c) c *= 2;
+  return c;
+}
+
+template <int RT> inline cudaError_t launch_outer_rt(OuterArgs p, int n_sms, bool dep, cudaStream_t st) {
+  p.slices0 = (p.side[0].d + kOutCols - 1) / kOutCols;
+  const int slices = p.slices0 + (p.side[1].d + kOutCols - 1) / kOutCols;
+  const int ctas = outer_ctas((long long)slices * p.n, n_sms, (long long)p.n_rows / p.n / (16 * kOutRowWarps));
+  const dim3 grid(slices, p.n, ctas), cl(1, 1, ctas);
+  return p.drop.thr16 ? launch_cluster(dep, adapter_outer_kernel<RT, true>, grid, cl, 2 * kOutQuads<RT> * 16, st, p)
+                      : launch_cluster(dep, adapter_outer_kernel<RT, false>, grid, cl, 2 * kOutQuads<RT> * 16, st, p);
+}
+inline cudaError_t launch_outer(bool bf, const OuterArgs& a, int n_sms, bool dep, cudaStream_t st) {
+  if (bf) switch (adapter_rank_tiles(a.r)) {
+      case 1: return launch_outer_rt<1>(a, n_sms, dep, st);
+      case 2: return launch_outer_rt<2>(a, n_sms, dep, st);
+      case 4: return launch_outer_rt<4>(a, n_sms, dep, st);
+      default: return launch_outer_rt<8>(a, n_sms, dep, st);
+    }
+  OuterArgs p = a;
+  p.slices0 = (p.side[0].d + kSimtOutCols - 1) / kSimtOutCols;
+  const int slices = p.slices0 + (p.side[1].d + kSimtOutCols - 1) / kSimtOutCols;
+  const int chunks = (p.r + kSimtRc - 1) / kSimtRc;
+  const int ctas = outer_ctas((long long)slices * p.n * chunks, n_sms, (long long)p.n_rows / p.n / (4 * kAdWarps));
+  const dim3 grid(slices, p.n * chunks, ctas), cl(1, 1, ctas);
+  return p.drop.thr16 ? launch_cluster(dep, adapter_outer_simt_kernel<true>, grid, cl, 0, st, p)
+                      : launch_cluster(dep, adapter_outer_simt_kernel<false>, grid, cl, 0, st, p);
+}
+
+}  // namespace cmoe

@@ -7,6 +7,8 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <atomic>
+#include <cmath>
 #include <cstdio>
 #include <cstring>
 #include <mutex>
@@ -14,9 +16,11 @@
 #include <type_traits>
 #include <vector>
 
+#include "adapters.cuh"
 #include "balance.cuh"
 #include "cluster.cuh"
 #include "combine.cuh"
+#include "dropout.cuh"
 #include "fp8.cuh"
 #include "common.cuh"
 #include "permute.cuh"
@@ -1360,6 +1364,300 @@ int cmoe_token_permute_static(const int32_t* topk_idx, int32_t n_rows, int32_t n
                        static_cast<cudaStream_t>(stream));
   CU_TRY(cudaGetLastError());
   return CMOE_OK;
+}
+
+}  // extern "C" (re-opened below)
+
+// ---------------------------------------------------------------------------
+// Low-rank adapters and dropout.
+namespace {
+
+// SMs of the current device; UNSUPPORTED where it is none of compute capability 10.x.
+int device_sms(int* n_sms) {
+  constexpr int kMost = 64;
+  static std::atomic<int> known[kMost];                  // a constant of the device
+  int dev = 0;
+  CU_TRY(cudaGetDevice(&dev));
+  if (dev < kMost && (*n_sms = known[dev].load(std::memory_order_relaxed)) > 0) return CMOE_OK;
+  int major = 0;
+  CU_TRY(cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev));
+  if (major != 10) return arg_fail(CMOE_ERR_UNSUPPORTED, "the device is not compute capability 10.x");
+  CU_TRY(cudaDeviceGetAttribute(n_sms, cudaDevAttrMultiProcessorCount, dev));
+  if (dev < kMost) known[dev].store(*n_sms, std::memory_order_relaxed);
+  return CMOE_OK;
+}
+
+struct Mat { const void* p; int64_t ld, cols; };
+
+// Whether two matrices of `rows` rows may share an element: column slices of one wider matrix do not.
+bool overlap(const Mat& a, const Mat& b, int64_t rows, int64_t esz) {
+  const auto pa = (intptr_t)a.p, pb = (intptr_t)b.p;
+  const int64_t ea = ((rows - 1) * a.ld + a.cols) * esz, eb = ((rows - 1) * b.ld + b.cols) * esz;
+  if (pa + ea <= pb || pb + eb <= pa) return false;
+  if (a.ld != b.ld) return true;
+  const int64_t line = a.ld * esz, off = (((int64_t)(pb - pa)) % line + line) % line;
+  return !(off >= a.cols * esz && off + b.cols * esz <= line);
+}
+bool same(const Mat& a, const Mat& b) { return a.p == b.p && a.ld == b.ld; }
+
+int check_drop(const cmoe_dropout_config* d, int64_t rows, Drop* out) {
+  *out = Drop{};
+  if (!d) return CMOE_OK;
+  if (!(d->p >= 0.0 && d->p < 1.0)) return arg_fail(CMOE_ERR_INVALID_ARG, "dropout: p outside [0, 1)");
+  const uint32_t thr = (uint32_t)std::floor(d->p * 65536.0 + 0.5);
+  if (thr > 65535u) return arg_fail(CMOE_ERR_INVALID_ARG, "dropout: p rounds to 1");
+  if (d->row0 < 0 || d->row0 > (int64_t)4294967296LL - rows) return arg_fail(CMOE_ERR_INVALID_ARG, "dropout: row0 + rows exceeds 2^32");
+  out->thr16 = thr << 16;
+  out->inv = (float)(65536.0 / (65536.0 - thr));
+  out->k0 = (uint32_t)d->seed; out->k1 = (uint32_t)(d->seed >> 32);
+  out->off0 = (uint32_t)d->offset; out->off1 = (uint32_t)(d->offset >> 32);
+  out->row0 = (uint32_t)d->row0;
+  return CMOE_OK;
+}
+
+int check_adapters(const cmoe_adapters* ad) {
+  if (!ad) return arg_fail(CMOE_ERR_INVALID_ARG, "null adapters");
+  if (ad->dtype != CMOE_BF16 && ad->dtype != CMOE_FP32) return arg_fail(CMOE_ERR_INVALID_ARG, "adapters: unknown dtype");
+  if (ad->n_adapters < 1 || ad->n_adapters > kAdMaxAdapters) return arg_fail(CMOE_ERR_INVALID_ARG, "adapters: n_adapters outside [1, 1024]");
+  if (ad->rank < 8 || ad->rank > kAdMaxRank || ad->rank % 8) return arg_fail(CMOE_ERR_INVALID_ARG, "adapters: rank is not a multiple of 8 in [8, 64]");
+  for (const int32_t d : {ad->d_in, ad->d_out})
+    if (d < 8 || d % 8 || d > (1 << 24)) return arg_fail(CMOE_ERR_INVALID_ARG, "adapters: d_in / d_out is not a multiple of 8 in [8, 2^24]");
+  return CMOE_OK;
+}
+
+int check_rows_mat(const Mat& m, int64_t esz, const char* what) {
+  if (!m.p) { snprintf(g_last_error, sizeof(g_last_error), "adapters: null %s", what); return CMOE_ERR_INVALID_ARG; }
+  if (m.ld < m.cols || m.ld > (1LL << 40) || (m.ld * esz) % 16 || ((uintptr_t)m.p & 15)) {
+    snprintf(g_last_error, sizeof(g_last_error), "adapters: %s: the row stride is below the width, or it or the pointer is no multiple of 16 bytes", what);
+    return CMOE_ERR_INVALID_ARG;
+  }
+  return CMOE_OK;
+}
+#define RC_TRY(expr)                      \
+  do {                                    \
+    const int rc_ = (expr);               \
+    if (rc_ != CMOE_OK) return rc_;       \
+  } while (0)
+
+// What both directions share once the arguments are known to be good.
+template <typename T> struct AdapterPass {
+  AdapterArgs<T> a{};
+  AdPlanOut plan{};
+  bool small = false;
+  int m = 0;
+  long long tiles = 0, live = 0;
+};
+
+template <typename T>
+int plan_adapter_pass(AdapterPass<T>& p, const cmoe_adapters* ad, const int32_t* row_adapter, int32_t n_rows, bool backward,
+                      void* scratch, int64_t scratch_bytes) {
+  constexpr bool bf = sizeof(T) == 2;
+  p.small = adapter_small(row_adapter, n_rows, backward);
+  p.m = adapter_tile_rows(bf, ad->rank, p.small && bf);
+  const bool planned = row_adapter && !p.small;
+  const AdapterScratch lay = adapter_scratch(bf, n_rows, ad->n_adapters, ad->rank, backward, !planned);
+  if (lay.total > 0) {
+    if (!scratch || ((uintptr_t)scratch & 255)) return arg_fail(CMOE_ERR_INVALID_ARG, "adapters: scratch null or not 256-byte aligned");
+    if (scratch_bytes < (int64_t)lay.total) return arg_fail(CMOE_ERR_CAPACITY, "adapters: scratch too small");
+  }
+  char* s = static_cast<char*>(scratch);
+  p.a.tiles.row_adapter = row_adapter;
+  p.a.n_rows = n_rows; p.a.n = ad->n_adapters; p.a.r = ad->rank; p.a.scale = ad->scale;
+  const int live_adapters = std::min(ad->n_adapters, n_rows);
+  if (planned) {
+    p.plan = {reinterpret_cast<int32_t*>(s + lay.tile_start), reinterpret_cast<int32_t*>(s + lay.tile_adapter),
+              reinterpret_cast<int32_t*>(s + lay.row_list)};
+    p.a.tiles.planned = 1;
+    p.a.tiles.tile_start = p.plan.tile_start; p.a.tiles.tile_adapter = p.plan.tile_adapter; p.a.tiles.row_list = p.plan.row_list;
+    p.tiles = adapter_max_tiles(n_rows, ad->n_adapters, p.m, false);
+    p.live = p.tiles;
+  } else if (p.small) {
+    p.tiles = n_rows;                                    // every row may head a tile
+    p.live = std::min<long long>(n_rows, live_adapters + n_rows / p.m);
+  } else {
+    p.tiles = p.live = adapter_max_tiles(n_rows, ad->n_adapters, p.m, true);
+  }
+  if (backward) { p.a.u_e = s + lay.u_e; p.a.u_z = s + lay.u_z; }
+  return CMOE_OK;
+}
+
+template <typename T>
+int adapter_forward_launch(const cmoe_adapters* ad, AdapterPass<T>& p, const Mat& x, const Mat& base, const Mat& out, float* z,
+                           const Drop& drop, int n_sms, cudaStream_t st) {
+  p.a.x = (const T*)x.p; p.a.ldx = x.ld;
+  p.a.w1 = (const T*)ad->a; p.a.w2 = (const T*)ad->b;
+  p.a.base = (const T*)base.p; p.a.ld_base = base.ld;
+  p.a.out = (T*)out.p; p.a.ld_out = out.ld;
+  p.a.z_out = z; p.a.d_k = ad->d_in; p.a.d_n = ad->d_out; p.a.drop = drop;
+  if (p.plan.row_list) CU_TRY(launch_adapter_plan(p.a, p.m, p.plan, st));
+  CU_TRY((launch_adapter<false>(p.a, p.small, p.tiles, p.live, n_sms, p.plan.row_list != nullptr, st)));
+  return CMOE_OK;
+}
+
+int check_adapter_forward(const cmoe_adapters* ad, const Mat& x, int32_t n_rows, const Mat& base, const Mat& out, const float* z) {
+  const int64_t esz = ad->dtype == CMOE_BF16 ? 2 : 4;
+  if (!ad->a || !ad->b || (((uintptr_t)ad->a | (uintptr_t)ad->b) & 15)) return arg_fail(CMOE_ERR_INVALID_ARG, "adapters: a / b null or not 16-byte aligned");
+  if (((uintptr_t)ad->scale | (uintptr_t)z) & 7) return arg_fail(CMOE_ERR_INVALID_ARG, "adapters: scale / z not 8-byte aligned");
+  RC_TRY(check_rows_mat(x, esz, "x"));
+  RC_TRY(check_rows_mat(out, esz, "out"));
+  if (base.p) RC_TRY(check_rows_mat(base, esz, "base"));
+  if (overlap(x, out, n_rows, esz)) return arg_fail(CMOE_ERR_INVALID_ARG, "adapters: x and out overlap");
+  if (base.p && !same(base, out) && overlap(base, out, n_rows, esz)) return arg_fail(CMOE_ERR_INVALID_ARG, "adapters: base and out overlap without being the same");
+  return CMOE_OK;
+}
+
+template <typename T>
+int adapter_forward_impl(const cmoe_adapters* ad, const Mat& x, const int32_t* row_adapter, int32_t n_rows, const Drop& drop, const Mat& base,
+                         const Mat& out, float* z, void* scratch, int64_t scratch_bytes, cudaStream_t st) {
+  AdapterPass<T> p;
+  RC_TRY(plan_adapter_pass(p, ad, row_adapter, n_rows, false, scratch, scratch_bytes));
+  int n_sms = 0;
+  RC_TRY(device_sms(&n_sms));
+  return adapter_forward_launch(ad, p, x, base, out, z, drop, n_sms, st);
+}
+
+template <typename T>
+int adapter_backward_impl(const cmoe_adapters* ad, const Mat& dy, const Mat& x, const float* z, const int32_t* row_adapter, int32_t n_rows,
+                          const Drop& drop, const Mat& dx_base, const Mat& dx, void* grad_a, void* grad_b, void* scratch,
+                          int64_t scratch_bytes, cudaStream_t st) {
+  AdapterPass<T> p;
+  RC_TRY(plan_adapter_pass(p, ad, row_adapter, n_rows, true, scratch, scratch_bytes));
+  int n_sms = 0;
+  RC_TRY(device_sms(&n_sms));
+  p.a.x = (const T*)dy.p; p.a.ldx = dy.ld;
+  p.a.w1 = (const T*)ad->b; p.a.w2 = (const T*)ad->a;
+  p.a.base = (const T*)dx_base.p; p.a.ld_base = dx_base.ld;
+  p.a.out = (T*)dx.p; p.a.ld_out = dx.ld;
+  p.a.z_in = z; p.a.d_k = ad->d_out; p.a.d_n = ad->d_in; p.a.drop = drop;
+  if (!grad_a) p.a.u_e = p.a.u_z = nullptr;
+  if (p.plan.row_list) CU_TRY(launch_adapter_plan(p.a, p.m, p.plan, st));
+  CU_TRY((launch_adapter<true>(p.a, false, p.tiles, p.live, n_sms, p.plan.row_list != nullptr, st)));
+  if (!grad_a) return CMOE_OK;
+  OuterArgs o{};
+  o.side[0] = {x.p, x.ld, p.a.u_e, grad_a, ad->d_in};
+  o.side[1] = {dy.p, dy.ld, p.a.u_z, grad_b, ad->d_out};
+  o.n_rows = n_rows; o.n = ad->n_adapters; o.r = ad->rank; o.m = p.m; o.tiles = p.a.tiles; o.drop = drop;
+  CU_TRY(launch_outer(sizeof(T) == 2, o, n_sms, true, st));
+  return CMOE_OK;
+}
+}  // namespace
+
+extern "C" {
+
+int cmoe_dropout(const void* x, int64_t ldx, const void* residual, int64_t ld_residual, int32_t rows, int32_t cols, int32_t dtype,
+                 const cmoe_dropout_config* drop, void* out, int64_t ld_out, void* stream) {
+  if (rows < 0 || cols < 0) return arg_fail(CMOE_ERR_INVALID_ARG, "dropout: negative size");
+  if (dtype != CMOE_BF16 && dtype != CMOE_FP32) return arg_fail(CMOE_ERR_INVALID_ARG, "dropout: unknown dtype");
+  if (!drop) return arg_fail(CMOE_ERR_INVALID_ARG, "dropout: null configuration");
+  Drop d;
+  RC_TRY(check_drop(drop, rows, &d));
+  if (rows == 0 || cols == 0) return CMOE_OK;
+  if (!x || !out) return arg_fail(CMOE_ERR_INVALID_ARG, "dropout: null x / out");
+  const int64_t esz = dtype == CMOE_BF16 ? 2 : 4;
+  const Mat mx{x, ldx, cols}, mr{residual, ld_residual, cols}, mo{out, ld_out, cols};
+  for (const Mat* m : {&mx, &mr, &mo})
+    if (m->p && (m->ld < cols || m->ld > (1LL << 40) || (uintptr_t)m->p % esz))
+      return arg_fail(CMOE_ERR_INVALID_ARG, "dropout: a row stride below the width, or a pointer that is not element-aligned");
+  if (!same(mx, mo) && overlap(mx, mo, rows, esz)) return arg_fail(CMOE_ERR_INVALID_ARG, "dropout: x and out overlap without being the same");
+  if (residual && !same(mr, mo) && overlap(mr, mo, rows, esz))
+    return arg_fail(CMOE_ERR_INVALID_ARG, "dropout: residual and out overlap without being the same");
+  int n_sms = 0;
+  RC_TRY(device_sms(&n_sms));
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (dtype == CMOE_BF16)
+    CU_TRY(launch_dropout(DropoutArgs<bf16>{(const bf16*)x, (const bf16*)residual, (bf16*)out, ldx, ld_residual, ld_out, rows, cols, d}, n_sms, st));
+  else
+    CU_TRY(launch_dropout(DropoutArgs<float>{(const float*)x, (const float*)residual, (float*)out, ldx, ld_residual, ld_out, rows, cols, d}, n_sms, st));
+  return CMOE_OK;
+}
+
+int64_t cmoe_adapter_scratch_bytes(const cmoe_adapters* ad, int32_t n_rows, int32_t with_row_adapter, int32_t backward) {
+  if (check_adapters(ad) != CMOE_OK || n_rows <= 0 || n_rows > kAdMaxRows) return 0;
+  const bool planned = with_row_adapter && (backward || n_rows > kAdSmallRows);
+  return (int64_t)adapter_scratch(ad->dtype == CMOE_BF16, n_rows, ad->n_adapters, ad->rank, backward != 0, !planned).total;
+}
+
+int cmoe_adapter_forward(const cmoe_adapters* ad, const void* x, int64_t ldx, const int32_t* row_adapter, int32_t n_rows,
+                         const cmoe_dropout_config* drop, const void* base, int64_t ld_base, void* out, int64_t ld_out, float* z,
+                         void* scratch, int64_t scratch_bytes, void* stream) {
+  RC_TRY(check_adapters(ad));
+  if (n_rows < 0) return arg_fail(CMOE_ERR_INVALID_ARG, "adapters: negative row count");
+  if (n_rows > kAdMaxRows) return arg_fail(CMOE_ERR_CAPACITY, "adapters: more than 2^30 rows");
+  Drop d;
+  RC_TRY(check_drop(drop, n_rows, &d));
+  if (n_rows == 0) return CMOE_OK;
+  const Mat mx{x, ldx, ad->d_in}, mb{base, ld_base, ad->d_out}, mo{out, ld_out, ad->d_out};
+  RC_TRY(check_adapter_forward(ad, mx, n_rows, mb, mo, z));
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  return ad->dtype == CMOE_BF16 ? adapter_forward_impl<bf16>(ad, mx, row_adapter, n_rows, d, mb, mo, z, scratch, scratch_bytes, st)
+                                : adapter_forward_impl<float>(ad, mx, row_adapter, n_rows, d, mb, mo, z, scratch, scratch_bytes, st);
+}
+
+int cmoe_adapter_backward(const cmoe_adapters* ad, const void* dy, int64_t ld_dy, const void* x, int64_t ldx, const float* z,
+                          const int32_t* row_adapter, int32_t n_rows, const cmoe_dropout_config* drop, const void* dx_base,
+                          int64_t ld_dx_base, void* dx, int64_t ld_dx, void* grad_a, void* grad_b, void* scratch,
+                          int64_t scratch_bytes, void* stream) {
+  RC_TRY(check_adapters(ad));
+  if (n_rows < 0) return arg_fail(CMOE_ERR_INVALID_ARG, "adapters: negative row count");
+  if (n_rows > kAdMaxRows) return arg_fail(CMOE_ERR_CAPACITY, "adapters: more than 2^30 rows");
+  Drop d;
+  RC_TRY(check_drop(drop, n_rows, &d));
+  if (!grad_a != !grad_b) return arg_fail(CMOE_ERR_INVALID_ARG, "adapters: grad_a and grad_b go together");
+  if (!grad_a && !dx) return arg_fail(CMOE_ERR_INVALID_ARG, "adapters: no gradient is wanted");
+  if (((uintptr_t)grad_a | (uintptr_t)grad_b) & 15) return arg_fail(CMOE_ERR_INVALID_ARG, "adapters: grad_a / grad_b not 16-byte aligned");
+  const int64_t esz = ad->dtype == CMOE_BF16 ? 2 : 4;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (n_rows == 0) {
+    if (grad_a) {
+      const size_t nr = (size_t)ad->n_adapters * ad->rank * esz;
+      CU_TRY(cudaMemsetAsync(grad_a, 0, nr * ad->d_in, st));
+      CU_TRY(cudaMemsetAsync(grad_b, 0, nr * ad->d_out, st));
+    }
+    return CMOE_OK;
+  }
+  if (!ad->a || !ad->b || (((uintptr_t)ad->a | (uintptr_t)ad->b) & 15)) return arg_fail(CMOE_ERR_INVALID_ARG, "adapters: a / b null or not 16-byte aligned");
+  if (((uintptr_t)ad->scale | (uintptr_t)z) & 7) return arg_fail(CMOE_ERR_INVALID_ARG, "adapters: scale / z not 8-byte aligned");
+  const Mat mdy{dy, ld_dy, ad->d_out}, mx{x, ldx, ad->d_in}, mb{dx ? dx_base : nullptr, ld_dx_base, ad->d_in}, mo{dx, ld_dx, ad->d_in};
+  RC_TRY(check_rows_mat(mdy, esz, "dy"));
+  if (grad_a) {
+    RC_TRY(check_rows_mat(mx, esz, "x"));
+    if (!z) return arg_fail(CMOE_ERR_INVALID_ARG, "adapters: null z");
+  }
+  if (dx) {
+    RC_TRY(check_rows_mat(mo, esz, "dx"));
+    if (overlap(mdy, mo, n_rows, esz)) return arg_fail(CMOE_ERR_INVALID_ARG, "adapters: dy and dx overlap");
+    if (grad_a && overlap(mx, mo, n_rows, esz)) return arg_fail(CMOE_ERR_INVALID_ARG, "adapters: x and dx overlap");
+  }
+  if (mb.p) {
+    RC_TRY(check_rows_mat(mb, esz, "dx_base"));
+    if (!same(mb, mo) && overlap(mb, mo, n_rows, esz)) return arg_fail(CMOE_ERR_INVALID_ARG, "adapters: dx_base and dx overlap without being the same");
+  }
+  return ad->dtype == CMOE_BF16
+             ? adapter_backward_impl<bf16>(ad, mdy, mx, z, row_adapter, n_rows, d, mb, mo, grad_a, grad_b, scratch, scratch_bytes, st)
+             : adapter_backward_impl<float>(ad, mdy, mx, z, row_adapter, n_rows, d, mb, mo, grad_a, grad_b, scratch, scratch_bytes, st);
+}
+
+int cmoe_ffn_forward_adapted(cmoe_layer* L, const void* x, int32_t T, const cmoe_adapters* ad, const int32_t* row_adapter,
+                             void* out, void* scratch, int64_t scratch_bytes, void* stream) {
+  if (!L) return arg_fail(CMOE_ERR_INVALID_ARG, "null layer");
+  RC_TRY(check_adapters(ad));
+  const int d = L->cfg.d_model;
+  if (ad->d_in != d || ad->d_out != d || ad->dtype != L->cfg.dtype)
+    return arg_fail(CMOE_ERR_INVALID_ARG, "adapters: d_in, d_out or dtype is not the layer's");
+  if (T <= 0) return cmoe_ffn_forward(L, x, T, out, stream);
+  const Mat mx{x, d, d}, mo{out, d, d};
+  RC_TRY(check_adapter_forward(ad, mx, T, mo, mo, nullptr));
+  int n_sms = 0;
+  RC_TRY(device_sms(&n_sms));
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const auto go = [&](auto pass) -> int {
+    RC_TRY(plan_adapter_pass(pass, ad, row_adapter, T, false, scratch, scratch_bytes));
+    RC_TRY(cmoe_ffn_forward(L, x, T, out, stream));
+    RC_TRY(adapter_forward_launch(ad, pass, mx, mo, mo, nullptr, Drop{}, n_sms, st));
+    L->launches += pass.plan.row_list ? 2 : 1;
+    return CMOE_OK;
+  };
+  return ad->dtype == CMOE_BF16 ? go(AdapterPass<bf16>{}) : go(AdapterPass<float>{});
 }
 
 const char* cmoe_status_string(int status) {
