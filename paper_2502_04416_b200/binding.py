@@ -6,7 +6,6 @@ from __future__ import annotations
 
 import ctypes as C
 import os
-from contextlib import nullcontext
 from typing import Dict, NamedTuple, Optional, Sequence
 
 import numpy as np
@@ -200,16 +199,20 @@ class Layer:
     def forward_adapted(self, x, a, b, row_adapter=None, scale=None, out=None, scratch=None, stream=None):
         """cmoe_ffn_forward_adapted: the forward of x [T,d] plus the low-rank adapter of every row
         (a, b, row_adapter, scale, scratch as in adapter_forward)."""
-        rows, d = _rows(x, "x")
-        ad = _adapters(x, a, b, scale)
-        ids = _adapter_ids(row_adapter, rows, x)
-        with _on(x, stream):
-            out = _out(out, "out", rows, d, x)
-            if d != self.d_model or not (x.is_contiguous() and out.is_contiguous()):
-                raise ValueError("x and out must be contiguous [T, d_model]")
-            scratch = _adapter_scratch(ad, rows, ids, 0, scratch, x)
-            st = load().cmoe_ffn_forward_adapted(self._h, x.data_ptr(), rows, C.byref(ad), ids, out.data_ptr(), _ptr(scratch),
-                                                 0 if scratch is None else scratch.numel(), _stream_ptr(None))
+        rows, d, ldx, dtype, dev = _rows(x, "x")
+        elsewhere = _elsewhere(dev, stream)
+        if elsewhere is not None:
+            with elsewhere:
+                return self.forward_adapted(x, a, b, row_adapter, scale, out, scratch)
+        ad = _adapters(dtype, dev, a, b, scale)
+        ids = _adapter_ids(row_adapter, rows, dev)
+        if out is None:
+            out = x.new_empty((rows, d))
+        if d != self.d_model or ldx != d or _matrix(out, "out", rows, d, dtype, dev) != d:
+            raise ValueError("x and out must be contiguous [T, d_model]")
+        scratch, s_ptr, s_bytes = _adapter_scratch(ad, rows, ids, 0, scratch, x)
+        st = load().cmoe_ffn_forward_adapted(self._h, x.data_ptr(), rows, C.byref(ad), ids, out.data_ptr(), s_ptr, s_bytes,
+                                             _current_stream(dev))
         _check(st, "cmoe_ffn_forward_adapted")
         return out
 
@@ -453,95 +456,99 @@ def _drop_config(drop: Optional[Dropout]):
     return None if drop is None else CmoeDropoutConfig(drop.p, drop.seed & 0xFFFFFFFFFFFFFFFF, drop.offset & 0xFFFFFFFFFFFFFFFF, drop.row0)
 
 
+def _matrix(t, what: str, rows: int, cols: int, dtype, dev: int) -> int:
+    """The row stride of a row-strided [rows, cols] matrix of this type and device."""
+    stride = t.stride()
+    if t.shape != (rows, cols) or t.dtype is not dtype or t.get_device() != dev or (stride[1] != 1 and cols > 1 and rows > 0):
+        raise ValueError(f"{what}: expected [{rows}, {cols}] of {dtype} on cuda:{dev} with neighbouring columns")
+    return stride[0] if rows > 1 else cols                     # the stride of a single row has no meaning
+
+
 def _rows(t, what: str):
-    """(rows, columns) of a row-strided CUDA matrix."""
-    if not t.is_cuda or t.dim() != 2:
+    """(rows, columns, row stride, type, device) of a row-strided CUDA matrix."""
+    dev = t.get_device()
+    if dev < 0 or t.dim() != 2:
         raise ValueError(f"{what}: a two-dimensional CUDA tensor is expected")
-    _matrix(t, what, t.shape[0], t.shape[1], t)
-    return t.shape
+    rows, cols = t.shape
+    return rows, cols, _matrix(t, what, rows, cols, t.dtype, dev), t.dtype, dev
 
 
-def _matrix(t, what: str, rows: int, cols: int, like) -> None:
-    """A row-strided matrix of the device and type of `like`."""
-    if t.shape != (rows, cols) or t.dtype != like.dtype or t.device != like.device or (cols > 1 and rows > 0 and t.stride(1) != 1):
-        raise ValueError(f"{what}: expected [{rows}, {cols}] of {like.dtype} on {like.device} with neighbouring columns")
+def _like(t, what: str, shape, dtype, dev: int) -> int:
+    """The address of a contiguous tensor of this shape, type and device."""
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != dev or not t.is_contiguous():
+        raise ValueError(f"{what}: expected a contiguous {list(shape)} of {dtype} on cuda:{dev}")
+    return t.data_ptr()
 
 
-def _ld(t) -> int:
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1]       # the stride of a single row has no meaning
-
-
-def _on(like, stream):
-    """A context in which the tensor's device is current and `stream` (None: that device's current one) takes the work,
-    allocations included, so that what the call frees is not handed to work of another stream."""
+def _elsewhere(dev: int, stream):
+    """None where the call's device is current and its work goes to that device's current stream, else a context in which
+    that holds: what the call allocates and frees then belongs to the stream that uses it."""
     import torch
     if stream is not None:
-        if stream.device != like.device:
+        if stream.device.index != dev:
             raise ValueError("the stream and the tensors are on different devices")
         return torch.cuda.stream(stream)
-    return nullcontext() if like.device.index == torch.cuda.current_device() else torch.cuda.device(like.device)
+    return None if torch.cuda.current_device() == dev else torch.cuda.device(dev)
 
 
-def _out(out, what: str, rows: int, cols: int, like):
-    if out is None:
-        import torch
-        return torch.empty((rows, cols), dtype=like.dtype, device=like.device)
-    _matrix(out, what, rows, cols, like)
-    return out
+def _current_stream(dev: int) -> int:
+    import torch
+    return torch._C._cuda_getCurrentRawStream(dev)             # torch.cuda.current_stream(dev).cuda_stream, without the objects
 
 
 def dropout(x, drop: Dropout, residual=None, out=None, stream=None):
     """cmoe_dropout on CUDA tensors [rows, cols] (rows may be strided): residual + keep * x / (1 - p).  The gradient by x is
     dropout(dout, drop)."""
-    rows, cols = _rows(x, "x")
+    rows, cols, ldx, dtype, dev = _rows(x, "x")
+    elsewhere = _elsewhere(dev, stream)
+    if elsewhere is not None:
+        with elsewhere:
+            return dropout(x, drop, residual, out)
     code = _dtype_code(x)
-    if residual is not None:
-        _matrix(residual, "residual", rows, cols, x)
-    cfg = _drop_config(drop)
-    with _on(x, stream):
-        out = _out(out, "out", rows, cols, x)
-        st = load().cmoe_dropout(x.data_ptr(), _ld(x), None if residual is None else residual.data_ptr(),
-                                 0 if residual is None else _ld(residual), rows, cols, code, C.byref(cfg),
-                                 out.data_ptr(), _ld(out), _stream_ptr(None))
-    _check(st, "cmoe_dropout")
+    ld_res = 0 if residual is None else _matrix(residual, "residual", rows, cols, dtype, dev)
+    if out is None:
+        out = x.new_empty((rows, cols))
+    ld_out = _matrix(out, "out", rows, cols, dtype, dev)
+    st = load().cmoe_dropout(x.data_ptr(), ldx, None if residual is None else residual.data_ptr(), ld_res, rows, cols, code,
+                             C.byref(_drop_config(drop)), out.data_ptr(), ld_out, _current_stream(dev))
+    if st:
+        _check(st, "cmoe_dropout")
     return out
 
 
-def _adapters(like, a, b, scale) -> CmoeAdapters:
+def _adapters(dtype, dev: int, a, b, scale) -> CmoeAdapters:
     n, r, d_in = a.shape
     d_out = b.shape[1]
-    for t, what, shape in ((a, "a", (n, r, d_in)), (b, "b", (n, d_out, r))):
-        if t.shape != shape or t.dtype != like.dtype or t.device != like.device or not t.is_contiguous():
-            raise ValueError(f"{what}: expected a contiguous {list(shape)} of {like.dtype} on {like.device}")
-    if scale is not None:
-        import torch
-        if scale.shape != (n,) or scale.dtype != torch.float32 or scale.device != like.device or not scale.is_contiguous():
-            raise ValueError("scale: expected a contiguous float32 tensor, one value per adapter")
-    return CmoeAdapters(n, r, d_in, d_out, _dtype_code(like), a.data_ptr(), b.data_ptr(), None if scale is None else scale.data_ptr())
+    import torch
+    code = CMOE_BF16 if dtype is torch.bfloat16 else CMOE_FP32 if dtype is torch.float32 else None
+    if code is None:
+        raise TypeError(f"unsupported dtype {dtype}")
+    return CmoeAdapters(n, r, d_in, d_out, code, _like(a, "a", (n, r, d_in), dtype, dev), _like(b, "b", (n, d_out, r), dtype, dev),
+                        None if scale is None else _like(scale, "scale", (n,), torch.float32, dev))
 
 
-def _adapter_ids(row_adapter, rows: int, like):
+def _adapter_ids(row_adapter, rows: int, dev: int):
     if row_adapter is None:
         return None
     import torch
-    if row_adapter.shape != (rows,) or row_adapter.dtype != torch.int32 or row_adapter.device != like.device or not row_adapter.is_contiguous():
-        raise ValueError("row_adapter: expected a contiguous int32 tensor, one number per row")
-    return row_adapter.data_ptr()
+    return _like(row_adapter, "row_adapter", (rows,), torch.int32, dev)
+
+
+ADAPTER_SMALL_ROWS = 256     # row counts up to which cmoe_adapter_forward needs no scratch
 
 
 def _adapter_scratch(ad: CmoeAdapters, rows: int, ids, backward: int, scratch, like):
-    """The scratch of a call; allocated here where the caller gives none."""
-    import torch
+    """(tensor, address, bytes) of the scratch of a call; allocated here where the caller gives none."""
     if scratch is None:
+        if not backward and (ids is None or rows <= ADAPTER_SMALL_ROWS):
+            return None, None, 0
+        import torch
         nbytes = load().cmoe_adapter_scratch_bytes(C.byref(ad), rows, 0 if ids is None else 1, backward)
-        return torch.empty(nbytes, dtype=torch.uint8, device=like.device) if nbytes else None
-    if scratch.device != like.device or not scratch.is_contiguous() or scratch.dtype != torch.uint8:
-        raise ValueError("scratch: expected a contiguous uint8 tensor on the device of the rows")
-    return scratch
-
-
-def _ptr(t):
-    return None if t is None else t.data_ptr()
+        scratch = like.new_empty((nbytes,), dtype=torch.uint8)
+        return scratch, scratch.data_ptr(), nbytes
+    import torch
+    n = scratch.numel()
+    return scratch, _like(scratch, "scratch", (n,), torch.uint8, like.get_device()), n
 
 
 def adapter_forward(x, a, b, row_adapter=None, scale=None, base=None, dropout: Optional[Dropout] = None, want_z: bool = False,
@@ -550,25 +557,30 @@ def adapter_forward(x, a, b, row_adapter=None, scale=None, base=None, dropout: O
     (outside [0, n): out[t] = base[t]; None: every row takes adapter 0).
     x [rows, d_in], base / out [rows, d_out] (rows may be strided), a [n, rank, d_in], b [n, d_out, rank], row_adapter int32
     [rows], scale float32 [n].  Returns out, or (out, z) with z float32 [rows, rank] for adapter_backward."""
+    rows, d_in, ldx, dtype, dev = _rows(x, "x")
+    elsewhere = _elsewhere(dev, stream)
+    if elsewhere is not None:
+        with elsewhere:
+            return adapter_forward(x, a, b, row_adapter, scale, base, dropout, want_z, out, z, scratch)
     import torch
-    rows, d_in = _rows(x, "x")
-    ad = _adapters(x, a, b, scale)
+    ad = _adapters(dtype, dev, a, b, scale)
     if d_in != ad.d_in:
         raise ValueError(f"x: expected rows of {ad.d_in}")
-    if base is not None:
-        _matrix(base, "base", rows, ad.d_out, x)
-    if z is not None and (z.shape != (rows, ad.rank) or z.dtype != torch.float32 or z.device != x.device or not z.is_contiguous()):
-        raise ValueError("z: expected a contiguous float32 [rows, rank]")
-    ids, cfg = _adapter_ids(row_adapter, rows, x), _drop_config(dropout)
-    with _on(x, stream):
-        out = _out(out, "out", rows, ad.d_out, x)
-        if z is None and want_z:
-            z = torch.empty((rows, ad.rank), dtype=torch.float32, device=x.device)
-        scratch = _adapter_scratch(ad, rows, ids, 0, scratch, x)
-        st = load().cmoe_adapter_forward(C.byref(ad), x.data_ptr(), _ld(x), ids, rows, None if cfg is None else C.byref(cfg),
-                                         _ptr(base), 0 if base is None else _ld(base), out.data_ptr(), _ld(out), _ptr(z),
-                                         _ptr(scratch), 0 if scratch is None else scratch.numel(), _stream_ptr(None))
-    _check(st, "cmoe_adapter_forward")
+    d_out = ad.d_out
+    ld_base = 0 if base is None else _matrix(base, "base", rows, d_out, dtype, dev)
+    ids = _adapter_ids(row_adapter, rows, dev)
+    if out is None:
+        out = x.new_empty((rows, d_out))
+    ld_out = _matrix(out, "out", rows, d_out, dtype, dev)
+    if z is None and want_z:
+        z = x.new_empty((rows, ad.rank), dtype=torch.float32)
+    z_ptr = None if z is None else _like(z, "z", (rows, ad.rank), torch.float32, dev)
+    scratch, s_ptr, s_bytes = _adapter_scratch(ad, rows, ids, 0, scratch, x)
+    st = load().cmoe_adapter_forward(C.byref(ad), x.data_ptr(), ldx, ids, rows, None if dropout is None else C.byref(_drop_config(dropout)),
+                                     None if base is None else base.data_ptr(), ld_base, out.data_ptr(), ld_out, z_ptr,
+                                     s_ptr, s_bytes, _current_stream(dev))
+    if st:
+        _check(st, "cmoe_adapter_forward")
     return out if z is None else (out, z)
 
 
@@ -576,36 +588,37 @@ def adapter_backward(dy, x, z, a, b, row_adapter=None, scale=None, dx_base=None,
                      want_dx: bool = True, want_grads: bool = True, dx=None, grad_a=None, grad_b=None, scratch=None, stream=None):
     """cmoe_adapter_backward on CUDA tensors: (dx, grad_a, grad_b) of adapter_forward's out for its gradient dy, with the
     forward's x, z, row_adapter, scale and dropout; dx_base is added to dx.  Gradients that are not wanted are None."""
+    rows, d_out, ld_dy, dtype, dev = _rows(dy, "dy")
+    elsewhere = _elsewhere(dev, stream)
+    if elsewhere is not None:
+        with elsewhere:
+            return adapter_backward(dy, x, z, a, b, row_adapter, scale, dx_base, dropout, want_dx, want_grads, dx, grad_a, grad_b, scratch)
     import torch
-    rows, d_out = _rows(dy, "dy")
-    ad = _adapters(dy, a, b, scale)
+    ad = _adapters(dtype, dev, a, b, scale)
     if d_out != ad.d_out:
         raise ValueError(f"dy: expected rows of {ad.d_out}")
-    want_dx, want_grads = want_dx or dx is not None, want_grads or grad_a is not None or grad_b is not None
-    if want_grads:
-        _matrix(x, "x", rows, ad.d_in, dy)
-        if z.shape != (rows, ad.rank) or z.dtype != torch.float32 or z.device != dy.device or not z.is_contiguous():
-            raise ValueError("z: expected a contiguous float32 [rows, rank]")
+    d_in = ad.d_in
+    ids = _adapter_ids(row_adapter, rows, dev)
+    ldx = ld_base = ld_dx = 0
+    x_ptr = z_ptr = dx_ptr = ga_ptr = gb_ptr = None
+    if want_dx or dx is not None:
+        if dx is None:
+            dx = dy.new_empty((rows, d_in))
+        ld_dx, dx_ptr = _matrix(dx, "dx", rows, d_in, dtype, dev), dx.data_ptr()
     if dx_base is not None:
-        _matrix(dx_base, "dx_base", rows, ad.d_in, dy)
-    for t, like in ((grad_a, a), (grad_b, b)):
-        if t is not None and (t.shape != like.shape or t.dtype != like.dtype or t.device != like.device or not t.is_contiguous()):
-            raise ValueError("grad_a / grad_b: expected contiguous tensors like a / b")
-    ids, cfg = _adapter_ids(row_adapter, rows, dy), _drop_config(dropout)
-    with _on(dy, stream):
-        if want_dx:
-            dx = _out(dx, "dx", rows, ad.d_in, dy)
-        if want_grads:
-            grad_a = torch.empty_like(a) if grad_a is None else grad_a
-            grad_b = torch.empty_like(b) if grad_b is None else grad_b
-        scratch = _adapter_scratch(ad, rows, ids, 1, scratch, dy)
-        st = load().cmoe_adapter_backward(C.byref(ad), dy.data_ptr(), _ld(dy), _ptr(x) if want_grads else None,
-                                          _ld(x) if want_grads else 0, _ptr(z) if want_grads else None, ids, rows,
-                                          None if cfg is None else C.byref(cfg), _ptr(dx_base),
-                                          0 if dx_base is None else _ld(dx_base), _ptr(dx), 0 if dx is None else _ld(dx),
-                                          _ptr(grad_a), _ptr(grad_b), _ptr(scratch), 0 if scratch is None else scratch.numel(),
-                                          _stream_ptr(None))
-    _check(st, "cmoe_adapter_backward")
+        ld_base = _matrix(dx_base, "dx_base", rows, d_in, dtype, dev)
+    if want_grads or grad_a is not None or grad_b is not None:
+        ldx, x_ptr, z_ptr = _matrix(x, "x", rows, d_in, dtype, dev), x.data_ptr(), _like(z, "z", (rows, ad.rank), torch.float32, dev)
+        grad_a = torch.empty_like(a) if grad_a is None else grad_a
+        grad_b = torch.empty_like(b) if grad_b is None else grad_b
+        ga_ptr, gb_ptr = _like(grad_a, "grad_a", a.shape, dtype, dev), _like(grad_b, "grad_b", b.shape, dtype, dev)
+    scratch, s_ptr, s_bytes = _adapter_scratch(ad, rows, ids, 1, scratch, dy)
+    st = load().cmoe_adapter_backward(C.byref(ad), dy.data_ptr(), ld_dy, x_ptr, ldx, z_ptr, ids, rows,
+                                      None if dropout is None else C.byref(_drop_config(dropout)),
+                                      None if dx_base is None else dx_base.data_ptr(), ld_base, dx_ptr, ld_dx, ga_ptr, gb_ptr,
+                                      s_ptr, s_bytes, _current_stream(dev))
+    if st:
+        _check(st, "cmoe_adapter_backward")
     return dx, grad_a, grad_b
 
 

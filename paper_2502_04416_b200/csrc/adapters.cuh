@@ -61,17 +61,25 @@ adapter_plan_kernel(const int32_t* row_adapter, int n_rows, int n, int m, const 
   for (int i = threadIdx.x; i < 32 * groups; i += blockDim.x) hist[i] = 0;
   __syncthreads();
   int32_t* mine = hist + warp * groups;
-  auto group_of = [&](long long row) {
-    if (row >= hi) return -1;
-    const int v = __ldcg(row_adapter + row);
-    return (unsigned)v < (unsigned)n ? v : n;
+  // the groups of 32 kBatch rows from r0 on, their loads in flight at once (-1 behind the warp's last row)
+  constexpr int kBatch = 8;
+  auto groups_of = [&](long long r0, int (&v)[kBatch]) {
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      const long long row = r0 + 32 * i + lane;
+      v[i] = row < hi ? __ldcg(row_adapter + row) : 0;
+      v[i] = row < hi ? ((unsigned)v[i] < (unsigned)n ? v[i] : n) : -1;
+    }
   };
-#pragma unroll 4
-  for (long long r0 = lo; r0 < hi; r0 += 32) {
-    const int g = group_of(r0 + lane);
-    const unsigned same = __match_any_sync(0xffffffffu, g);
-    if (g >= 0 && (same & lt) == 0) mine[g] += __popc(same);
-    __syncwarp();
+  for (long long r0 = lo; r0 < hi; r0 += 32 * kBatch) {
+    int v[kBatch];
+    groups_of(r0, v);
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      const unsigned same = __match_any_sync(0xffffffffu, v[i]);
+      if (v[i] >= 0 && (same & lt) == 0) mine[v[i]] += __popc(same);
+      __syncwarp();
+    }
   }
   __syncthreads();
   for (int g = threadIdx.x; g < groups; g += blockDim.x) {
@@ -93,17 +101,21 @@ adapter_plan_kernel(const int32_t* row_adapter, int n_rows, int n, int m, const 
     o.tile_adapter[t] = a;
     for (int i = max(0, count[a] - (t - start[a]) * m); i < m; ++i) o.row_list[(size_t)t * m + i] = -1;
   }
-#pragma unroll 4
-  for (long long r0 = lo; r0 < hi; r0 += 32) {
-    const int g = group_of(r0 + lane);
-    const unsigned same = __match_any_sync(0xffffffffu, g);
-    const int before = g >= 0 ? mine[g] : 0;
-    __syncwarp();
-    if (g >= 0) {
-      o.row_list[(size_t)start[g] * m + before + __popc(same & lt)] = (int32_t)(r0 + lane);
-      if ((same & lt) == 0) mine[g] = before + __popc(same);
+  for (long long r0 = lo; r0 < hi; r0 += 32 * kBatch) {
+    int v[kBatch];
+    groups_of(r0, v);
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      const int g = v[i];
+      const unsigned same = __match_any_sync(0xffffffffu, g);
+      const int before = g >= 0 ? mine[g] : 0;
+      __syncwarp();
+      if (g >= 0) {
+        o.row_list[(size_t)start[g] * m + before + __popc(same & lt)] = (int32_t)(r0 + 32 * i + lane);
+        if ((same & lt) == 0) mine[g] = before + __popc(same);
+      }
+      __syncwarp();
     }
-    __syncwarp();
   }
 }
 inline size_t adapter_plan_smem(int n) { return (size_t)(35 * (n + 1) + 1 + 32) * sizeof(int32_t); }
@@ -166,6 +178,7 @@ template <typename T> struct AdapterArgs {
   const float* z_in;                     // backward: the forward's z, for the operand of dB
   void *u_e, *u_z;                       // backward: s e / (1 - p) and s z in the order of the tiles, or null
   int n_rows, n, r, d_k, d_n;
+  int wide_x, wide_n;                    // rows of x and w1's, of base and out, on 32-byte boundaries and of whole 32-byte pieces
   AdTiles tiles;
   Drop drop;
 };
@@ -229,22 +242,60 @@ __device__ __forceinline__ void adapter_none(const AdapterArgs<T>& p, const int3
 
 // ---- bf16 -------------------------------------------------------------------------------------------------------------
 // MT: 16-row MMA tiles of a row tile; RT: 8-wide tiles of the rank (padded with zeros); TRANS: backward.
-// Shared memory: part (the sums of four warps), recv (those of every block of the cluster), the middle as two bf16.
-template <int MT, int RT> struct AdapterSmem {
-  static constexpr int kM = 16 * MT, kR = 8 * RT, kStride = kR + 8;
-  static constexpr int kPart = 4 * kM * kR * 4, kRecv = kM * kR * 4, kMid = 2 * kM * kStride * 2;
+//
+// A lane of an 8 x 4 fragment loads 32 neighbouring bytes of its row: four lanes make whole 128-byte lines, and 32 bytes are
+// the operands of four k steps (k inside a 64-wide block is permuted alike on both sides, which leaves the sums as they are)
+// or eight tiles' results of one lane.  Loads that are 16 bytes wide, or go by way of shared memory, are bound by L1 instead of
+// HBM (16384 rows x 4096, rank 16, rows in and out: 106 us through a ring of asynchronous copies, L1 76 % busy).  What is in
+// flight is left to the number of resident warps.  At ranks above 32 two warps share the rows and split the rank.
+template <int MT, int RT, bool TRANS> struct AdapterShape {
+  static constexpr int kM = 16 * MT, kR = 8 * RT;
+  static constexpr int kSplit = RT == 8 ? 2 : 1, kRtw = RT / kSplit, kGroups = kAdWarps / kSplit;   // warps of a rank's share
+  static constexpr int kQuads = MT * RT * 32;
+  // elements between the middle's rows: no two of a fragment's lanes meet in a bank
+  static constexpr int kStride = TRANS ? (RT == 1 ? 8 : kR + 8) : RT == 8 ? 96 : kR;
+  static constexpr int kPart = kGroups / 2 * kQuads * 16, kRecv = kQuads * 16, kMid = 2 * kM * kStride * 2;
   static constexpr int bytes(int ctas) { return kPart + ctas * kRecv + kMid + kM * 4; }
+  static constexpr int kMinBlocks = MT == 1 ? (RT <= 2 ? 3 : 2) : RT == 8 ? 1 : 2;
 };
 
+// 32 bytes in two halves; zeros where a half is not wanted.  wide: the row starts on a 32-byte boundary and both halves go together.
+template <bool STREAM>
+__device__ __forceinline__ void ld32(const bf16* p, bool wide, bool in0, bool in1, uint32_t (&r)[8]) {
+  if (wide) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r[i] = 0u;
+    if (in0) {
+      if (STREAM) ld256_stream(p, r);
+      else
+        asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                     : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "l"(p) : "memory");
+    }
+  } else {
+    const uint4 zero = make_uint4(0u, 0u, 0u, 0u), a = in0 ? ld_dep16(p) : zero, b = in1 ? ld_dep16(p + 8) : zero;
+    r[0] = a.x; r[1] = a.y; r[2] = a.z; r[3] = a.w; r[4] = b.x; r[5] = b.y; r[6] = b.z; r[7] = b.w;
+  }
+}
+__device__ __forceinline__ void drop16(uint32_t (&r)[8], const Drop& d, uint32_t row, uint32_t block) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const uint4 w = drop_draws(d, row, block + h);
+    r[4 * h] = drop_pair(r[4 * h], w.x, d.thr16);
+    r[4 * h + 1] = drop_pair(r[4 * h + 1], w.y, d.thr16);
+    r[4 * h + 2] = drop_pair(r[4 * h + 2], w.z, d.thr16);
+    r[4 * h + 3] = drop_pair(r[4 * h + 3], w.w, d.thr16);
+  }
+}
+
 template <int MT, int RT, bool TRANS, bool DROP>
-__global__ void __launch_bounds__(kAdThreads, MT * RT <= 8 ? 2 : 1)
+__global__ void __launch_bounds__(kAdThreads, AdapterShape<MT, RT, TRANS>::kMinBlocks)
 adapter_kernel(const AdapterArgs<bf16> p) {
-  using S = AdapterSmem<MT, RT>;
-  constexpr int M = S::kM, kStride = S::kStride, kQuads = MT * RT * 32;
+  using S = AdapterShape<MT, RT, TRANS>;
+  constexpr int M = S::kM, kStride = S::kStride, kQuads = S::kQuads, kRtw = S::kRtw, kGroups = S::kGroups;
   extern __shared__ __align__(16) uint8_t smem[];
   const uint32_t ctas = cluster_ctas(), rank = cluster_rank();
-  float4* part = reinterpret_cast<float4*>(smem);                              // [4][MT][RT][lane]
-  float4* recv = part + 4 * kQuads;                                            // [ctas][MT][RT][lane]
+  float4* part = reinterpret_cast<float4*>(smem);                              // [kGroups / 2][MT][RT][lane]
+  float4* recv = part + kGroups / 2 * kQuads;                                  // [ctas][MT][RT][lane]
   uint16_t* mid = reinterpret_cast<uint16_t*>(recv + ctas * kQuads);           // [high, low][M][kStride]
   int32_t* rows = reinterpret_cast<int32_t*>(mid + 2 * M * kStride);
   rc_cluster_arrive();                                                         // this block has started
@@ -258,18 +309,6 @@ adapter_kernel(const AdapterArgs<bf16> p) {
     return;
   }
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
-  const int wi = (int)rank * kAdWarps + warp, nw = (int)ctas * kAdWarps;
-  const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
-
-  // ---- first product: [M, d_k] x [d_k, r], 32-wide blocks of d_k dealt to the warps of the cluster
-  float acc[MT][RT][4];
-#pragma unroll
-  for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) acc[mt][rt][i] = 0.0f;
-  const bf16* xr[MT][2];
   int row_of[MT][2];
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt)
@@ -277,129 +316,126 @@ adapter_kernel(const AdapterArgs<bf16> p) {
     for (int h = 0; h < 2; ++h) {
       const int row = rows[mt * 16 + 8 * h + g];
       row_of[mt][h] = row < 0 ? rows[0] : row;           // a row's sums are its own: rows past the end repeat the first
-      xr[mt][h] = p.x + (size_t)row_of[mt][h] * p.ldx + 8 * q;
     }
+
+  // ---- first product: [M, d_k] x [d_k, r], 64-wide blocks of d_k dealt to the warps of the cluster
+  const int kg = warp / S::kSplit, rt0 = (warp % S::kSplit) * kRtw;
+  float acc[MT][kRtw][4];
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+    for (int rt = 0; rt < kRtw; ++rt)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) acc[mt][rt][i] = 0.0f;
   const bf16* w1 = p.w1 + (size_t)a * p.r * p.d_k;
-  const int kb_end = (p.d_k + 31) >> 5;
-  struct Step { uint4 x[MT][2]; uint32_t w[RT][4]; };
-  auto load_step = [&](int kb, Step& s) {
-    const bool in = kb * 32 + 8 * q < p.d_k;
+#pragma unroll 1
+  for (int kb = (int)rank * kGroups + kg; kb * 64 < p.d_k; kb += (int)ctas * kGroups) {
+    const int k = kb * 64 + 16 * q;
+    const bool in0 = k < p.d_k, in1 = k + 8 < p.d_k;
+    uint32_t x[MT][2][8], w[kRtw][8];
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-      for (int h = 0; h < 2; ++h) s.x[mt][h] = in ? ld_dep16(xr[mt][h] + kb * 32) : zero;
+      for (int h = 0; h < 2; ++h) ld32<S::kSplit == 1>(p.x + (size_t)row_of[mt][h] * p.ldx + k, p.wide_x, in0, in1, x[mt][h]);
     if (!TRANS) {
 #pragma unroll
-      for (int rt = 0; rt < RT; ++rt) {
-        const uint4 v = in && rt * 8 + g < p.r ? ld_dep16(w1 + (size_t)(rt * 8 + g) * p.d_k + kb * 32 + 8 * q) : zero;
-        s.w[rt][0] = v.x; s.w[rt][1] = v.y; s.w[rt][2] = v.z; s.w[rt][3] = v.w;
+      for (int rt = 0; rt < kRtw; ++rt) {
+        const int n = (rt0 + rt) * 8 + g;
+        ld32<false>(w1 + (size_t)n * p.d_k + k, p.wide_x, in0 && n < p.r, in1 && n < p.r, w[rt]);
       }
     } else {
-      // rows of [d_k][r]: matrix i holds k = 8 (g / 2) + 2 i + g % 2, so that transposed it holds a lane's k = 8 q + 2 i, + 1
+      // rows of [d_k][r]: matrix i holds k = 16 (g / 2) + 2 i + g % 2, so that transposed it holds a lane's k = 16 q + 2 i, + 1
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int k = kb * 32 + 8 * (g >> 1) + 2 * i + (g & 1);
-        const bf16* wr = w1 + (size_t)k * p.r;
+      for (int i = 0; i < 8; ++i) {
+        const int kk = kb * 64 + 16 * (g >> 1) + 2 * i + (g & 1);
+        const bf16* wr = w1 + (size_t)kk * p.r;
         if (RT == 1) {
-          s.w[0][i] = k < p.d_k ? ld4(wr + 2 * q) : 0u;
+          w[0][i] = kk < p.d_k ? ld4(wr + 2 * q) : 0u;
         } else if (RT == 2) {
-          const uint2 v = k < p.d_k ? ld8(wr + 4 * q) : make_uint2(0u, 0u);
-          s.w[0][i] = v.x; s.w[RT - 1][i] = v.y;
+          const uint2 v = kk < p.d_k ? ld8(wr + 4 * q) : make_uint2(0u, 0u);
+          w[0][i] = v.x; w[kRtw - 1][i] = v.y;
         } else {
-#pragma unroll
-          for (int h = 0; h < RT / 4; ++h) {
-            const uint4 v = k < p.d_k && 32 * h + 8 * q < p.r ? ld_dep16(wr + 32 * h + 8 * q) : zero;
-            s.w[(4 * h) % RT][i] = v.x; s.w[(4 * h + 1) % RT][i] = v.y; s.w[(4 * h + 2) % RT][i] = v.z; s.w[(4 * h + 3) % RT][i] = v.w;
-          }
+          const uint4 v = kk < p.d_k && rt0 * 8 + 8 * q < p.r ? ld_dep16(wr + rt0 * 8 + 8 * q) : make_uint4(0u, 0u, 0u, 0u);
+          w[0][i] = v.x; w[1 % kRtw][i] = v.y; w[2 % kRtw][i] = v.z; w[3 % kRtw][i] = v.w;
         }
       }
-    }
-  };
-  auto use_step = [&](int kb, Step& s) {
-    if (TRANS) {
 #pragma unroll
-      for (int rt = 0; rt < RT; ++rt)
+      for (int rt = 0; rt < kRtw; ++rt)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) s.w[rt][i] = transpose8(s.w[rt][i]);
+        for (int i = 0; i < 8; ++i) w[rt][i] = transpose8(w[rt][i]);
     }
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
       if (DROP && !TRANS)
 #pragma unroll
-        for (int h = 0; h < 2; ++h) s.x[mt][h] = drop8(s.x[mt][h], drop_draws(p.drop, row_of[mt][h], kb * 4 + q), p.drop.thr16);
-      const uint4 lo = s.x[mt][0], hi = s.x[mt][1];
+        for (int h = 0; h < 2; ++h) drop16(x[mt][h], p.drop, row_of[mt][h], k >> 3);
 #pragma unroll
-      for (int rt = 0; rt < RT; ++rt) {
-        mma_bf16_16816(acc[mt][rt], lo.x, hi.x, lo.y, hi.y, s.w[rt][0], s.w[rt][1]);
-        mma_bf16_16816(acc[mt][rt], lo.z, hi.z, lo.w, hi.w, s.w[rt][2], s.w[rt][3]);
-      }
-    }
-  };
-  {
-    Step cur, nxt;
-    if (wi < kb_end) load_step(wi, cur);
-#pragma unroll 1
-    for (int kb = wi; kb < kb_end; kb += nw) {
-      if (kb + nw < kb_end) load_step(kb + nw, nxt);
-      use_step(kb, cur);
-      cur = nxt;
+      for (int rt = 0; rt < kRtw; ++rt)
+#pragma unroll
+        for (int s = 0; s < 4; ++s)
+          mma_bf16_16816(acc[mt][rt], x[mt][0][2 * s], x[mt][1][2 * s], x[mt][0][2 * s + 1], x[mt][1][2 * s + 1], w[rt][2 * s], w[rt][2 * s + 1]);
     }
   }
 
-  // ---- second product's operands of this warp's first 32 columns: in flight while the sums meet
+  // ---- second product's operands, 64 columns a warp at a time
   const bf16* w2 = p.w2 + (size_t)a * p.r * p.d_n;
-  const int nb_end = p.out ? (p.d_n + 31) >> 5 : 0;
-  struct Cols { uint32_t w[4][RT]; uint4 base[MT][2]; };
-  auto load_cols = [&](int nb, Cols& s) {
+  const int nb0 = (int)rank * kAdWarps + warp, n_cols = p.out ? p.d_n : 0;
+  uint32_t base[MT][2][8], w[4][RT];
+  auto load_base = [&](int nb) {
+    const int c = nb * 64 + 16 * q;
+    const bool in0 = p.base && c < p.d_n, in1 = p.base && c + 8 < p.d_n;
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) ld32<true>(p.base + (size_t)row_of[mt][h] * p.ld_base + c, p.wide_n, in0, in1, base[mt][h]);
+  };
+  // half 0: the lanes' columns 16 q .. 16 q + 7 (tiles 0 .. 3), half 1: the other eight (4 .. 7)
+  auto load_w = [&](int nb, int half) {
     if (!TRANS) {
-      // tile j's column g stands for column 8 (g / 2) + 2 j + g % 2, so that a lane's results are columns 8 q .. 8 q + 7
+      // tile j's column g stands for column 16 (g / 2) + 2 j + g % 2, so that a lane's results are neighbours
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const int c = nb * 32 + 8 * (g >> 1) + 2 * j + (g & 1);
+        const int c = nb * 64 + 16 * (g >> 1) + 8 * half + 2 * j + (g & 1);
         const bf16* wr = w2 + (size_t)c * p.r;
         if (RT == 1) {
-          s.w[j][0] = c < p.d_n ? ld4(wr + 2 * q) : 0u;
+          w[j][0] = c < p.d_n ? ld4(wr + 2 * q) : 0u;
         } else if (RT == 2) {
           const uint2 v = c < p.d_n ? ld8(wr + 4 * q) : make_uint2(0u, 0u);
-          s.w[j][0] = v.x; s.w[j][RT - 1] = v.y;
+          w[j][0] = v.x; w[j][RT - 1] = v.y;
         } else {
 #pragma unroll
           for (int h = 0; h < RT / 4; ++h) {
-            const uint4 v = c < p.d_n && 32 * h + 8 * q < p.r ? ld_dep16(wr + 32 * h + 8 * q) : zero;
-            s.w[j][(4 * h) % RT] = v.x; s.w[j][(4 * h + 1) % RT] = v.y; s.w[j][(4 * h + 2) % RT] = v.z; s.w[j][(4 * h + 3) % RT] = v.w;
+            const uint4 v = c < p.d_n && 32 * h + 8 * q < p.r ? ld_dep16(wr + 32 * h + 8 * q) : make_uint4(0u, 0u, 0u, 0u);
+            w[j][(4 * h) % RT] = v.x; w[j][(4 * h + 1) % RT] = v.y; w[j][(4 * h + 2) % RT] = v.z; w[j][(4 * h + 3) % RT] = v.w;
           }
         }
       }
     } else {
+      const int c = nb * 64 + 16 * q + 8 * half;
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt) {
-        const uint4 v = rt * 8 + g < p.r && nb * 32 + 8 * q < p.d_n ? ld_dep16(w2 + (size_t)(rt * 8 + g) * p.d_n + nb * 32 + 8 * q) : zero;
-        s.w[0][rt] = v.x; s.w[1][rt] = v.y; s.w[2][rt] = v.z; s.w[3][rt] = v.w;
+        const uint4 v = rt * 8 + g < p.r && c < p.d_n ? ld_dep16(w2 + (size_t)(rt * 8 + g) * p.d_n + c) : make_uint4(0u, 0u, 0u, 0u);
+        w[0][rt] = v.x; w[1][rt] = v.y; w[2][rt] = v.z; w[3][rt] = v.w;
       }
     }
-#pragma unroll
-    for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-        s.base[mt][h] = p.base && nb * 32 + 8 * q < p.d_n ? ld_dep16(p.base + (size_t)row_of[mt][h] * p.ld_base + nb * 32 + 8 * q) : zero;
   };
-  Cols cur;
-  if (wi < nb_end) load_cols(wi, cur);
+  if (MT == 1 && nb0 * 64 < n_cols) { load_base(nb0); load_w(nb0, 0); }        // few rows: in flight while the sums meet
 
-  // ---- the sums of eight warps, then of the cluster's blocks, each in a fixed order
-  if (warp >= 4)
+  // ---- the sums of the block's warps, then of the cluster's blocks, each in a fixed order
+  auto quad = [&](int mt, int rt) { return (mt * RT + rt0 + rt) * 32 + lane; };
+  if (kg >= kGroups / 2)
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-      for (int rt = 0; rt < RT; ++rt)
-        part[(warp - 4) * kQuads + (mt * RT + rt) * 32 + lane] = make_float4(acc[mt][rt][0], acc[mt][rt][1], acc[mt][rt][2], acc[mt][rt][3]);
+      for (int rt = 0; rt < kRtw; ++rt)
+        part[(kg - kGroups / 2) * kQuads + quad(mt, rt)] = make_float4(acc[mt][rt][0], acc[mt][rt][1], acc[mt][rt][2], acc[mt][rt][3]);
   __syncthreads();
-  if (warp < 4)
+  if (kg < kGroups / 2)
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-      for (int rt = 0; rt < RT; ++rt) {
-        float4& s = part[warp * kQuads + (mt * RT + rt) * 32 + lane];
+      for (int rt = 0; rt < kRtw; ++rt) {
+        float4& s = part[kg * kQuads + quad(mt, rt)];
         s = make_float4(s.x + acc[mt][rt][0], s.y + acc[mt][rt][1], s.z + acc[mt][rt][2], s.w + acc[mt][rt][3]);
       }
   __syncthreads();
@@ -407,7 +443,7 @@ adapter_kernel(const AdapterArgs<bf16> p) {
   for (int i = threadIdx.x; i < kQuads; i += kAdThreads) {
     float4 s = part[i];
 #pragma unroll
-    for (int w = 1; w < 4; ++w) {
+    for (int w = 1; w < kGroups / 2; ++w) {
       const float4 v = part[w * kQuads + i];
       s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
     }
@@ -463,62 +499,83 @@ adapter_kernel(const AdapterArgs<bf16> p) {
   }
 
   // ---- second product: [M, r] x [r, d_n], added to base
-  auto ld_mid4 = [&](int part_, int m, int c) { return *reinterpret_cast<const uint32_t*>(mid + (part_ * M + m) * kStride + c); };
 #pragma unroll 1
-  for (int nb = wi; nb < nb_end; nb += nw) {
-    Cols nxt;
-    if (nb + nw < nb_end) load_cols(nb + nw, nxt);
-    if (TRANS) {
+  for (int nb = nb0; nb * 64 < n_cols; nb += (int)ctas * kAdWarps) {
+    if (MT > 1 || nb != nb0) load_base(nb);
+    const int c = nb * 64 + 16 * q;
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
+    for (int half = 0; half < 2; ++half) {
+      if (MT > 1 || nb != nb0 || half == 1) load_w(nb, half);
+      if (TRANS) {
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt) cur.w[j][rt] = transpose8(cur.w[j][rt]);
-    }
-    const int c = nb * 32 + 8 * q;
+        for (int j = 0; j < 4; ++j)
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt) {
-      float o[4][4];
+          for (int rt = 0; rt < RT; ++rt) w[j][rt] = transpose8(w[j][rt]);
+      }
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
+      for (int mt = 0; mt < MT; ++mt) {
+        float o[4][4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) o[j][i] = 0.0f;
-      const int m0 = mt * 16 + g, m1 = m0 + 8;
-      if (RT == 1) {                               // one MMA: k 0 .. 7 the high part, 8 .. 15 the low part
-        const uint32_t a0 = ld_mid4(0, m0, 2 * q), a1 = ld_mid4(0, m1, 2 * q), a2 = ld_mid4(1, m0, 2 * q), a3 = ld_mid4(1, m1, 2 * q);
+        for (int j = 0; j < 4; ++j)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) mma_bf16_16816(o[j], a0, a1, a2, a3, cur.w[j][0], cur.w[j][0]);
-      } else {
+          for (int i = 0; i < 4; ++i) o[j][i] = 0.0f;
+        const uint16_t* m0 = mid + (mt * 16 + g) * kStride;
+        const uint16_t* m1 = m0 + 8 * kStride;
+        if (RT == 1) {                               // one MMA: k 0 .. 7 the high part, 8 .. 15 the low part
+          const uint32_t a0 = *reinterpret_cast<const uint32_t*>(m0 + 2 * q), a1 = *reinterpret_cast<const uint32_t*>(m1 + 2 * q);
+          const uint32_t a2 = *reinterpret_cast<const uint32_t*>(m0 + M * kStride + 2 * q), a3 = *reinterpret_cast<const uint32_t*>(m1 + M * kStride + 2 * q);
 #pragma unroll
-        for (int s = 0; s < RT / 2; ++s) {
-          // k of step s: ranks 16 s .. 16 s + 15 as they lie (TRANS), else a lane's own four neighbours
-          const int c0 = TRANS ? 16 * s + 2 * q : RT == 2 ? 4 * q : (s >> 1) * 32 + 8 * q + 4 * (s & 1);
-          const int c1 = TRANS ? c0 + 8 : c0 + 2;
+          for (int j = 0; j < 4; ++j) mma_bf16_16816(o[j], a0, a1, a2, a3, w[j][0], w[j][0]);
+        } else {
 #pragma unroll
-          for (int lo = 1; lo >= 0; --lo) {
-            const uint32_t a0 = ld_mid4(lo, m0, c0), a1 = ld_mid4(lo, m1, c0), a2 = ld_mid4(lo, m0, c1), a3 = ld_mid4(lo, m1, c1);
+          for (int s = 0; s < RT / 2; ++s)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) mma_bf16_16816(o[j], a0, a1, a2, a3, cur.w[j][(2 * s) % RT], cur.w[j][(2 * s + 1) % RT]);
+            for (int lo = 1; lo >= 0; --lo) {
+              // k of step s: ranks 16 s .. 16 s + 15 as they lie (TRANS), else a lane's own four neighbours
+              uint2 u0, u1;
+              if (TRANS) {
+                const uint16_t *s0 = m0 + lo * M * kStride + 16 * s + 2 * q, *s1 = m1 + lo * M * kStride + 16 * s + 2 * q;
+                u0 = make_uint2(*reinterpret_cast<const uint32_t*>(s0), *reinterpret_cast<const uint32_t*>(s0 + 8));
+                u1 = make_uint2(*reinterpret_cast<const uint32_t*>(s1), *reinterpret_cast<const uint32_t*>(s1 + 8));
+              } else {
+                const int at = lo * M * kStride + (RT == 2 ? 4 * q : (s >> 1) * 32 + 8 * q + 4 * (s & 1));
+                u0 = *reinterpret_cast<const uint2*>(m0 + at);
+                u1 = *reinterpret_cast<const uint2*>(m1 + at);
+              }
+#pragma unroll
+              for (int j = 0; j < 4; ++j) mma_bf16_16816(o[j], u0.x, u1.x, u0.y, u1.y, w[j][(2 * s) % RT], w[j][(2 * s + 1) % RT]);
+            }
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          float v[8];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) { v[2 * j] = o[j][2 * h]; v[2 * j + 1] = o[j][2 * h + 1]; }
+          if (DROP && TRANS) drop8(v, drop_draws(p.drop, row_of[mt][h], (c >> 3) + half), p.drop.thr16);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            uint32_t& b = base[mt][h][4 * half + j];
+            b = pack_bf16x2(v[2 * j] + __uint_as_float(b << 16), v[2 * j + 1] + __uint_as_float(b & 0xffff0000u));
           }
         }
       }
+    }
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const int row = rows[mt * 16 + 8 * h + g];
+        const uint32_t (&b)[8] = base[mt][h];
+        bf16* o = p.out + (size_t)row * p.ld_out + c;
         if (row < 0 || c >= p.d_n) continue;
-        float v[8];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) { v[2 * j] = o[j][2 * h]; v[2 * j + 1] = o[j][2 * h + 1]; }
-        if (DROP && TRANS) drop8(v, drop_draws(p.drop, row, c >> 3), p.drop.thr16);
-        const uint32_t b[4] = {cur.base[mt][h].x, cur.base[mt][h].y, cur.base[mt][h].z, cur.base[mt][h].w};
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          v[2 * j] += __uint_as_float(b[j] << 16);
-          v[2 * j + 1] += __uint_as_float(b[j] & 0xffff0000u);
+        if (p.wide_n) {
+          asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(o), "r"(b[0]), "r"(b[1]), "r"(b[2]), "r"(b[3]),
+                       "r"(b[4]), "r"(b[5]), "r"(b[6]), "r"(b[7]) : "memory");
+        } else {
+          *reinterpret_cast<uint4*>(o) = make_uint4(b[0], b[1], b[2], b[3]);
+          if (c + 8 < p.d_n) *reinterpret_cast<uint4*>(o + 8) = make_uint4(b[4], b[5], b[6], b[7]);
         }
-        store8(p.out + (size_t)row * p.ld_out + c, v);
       }
-    }
-    cur = nxt;
   }
 }
 
@@ -532,7 +589,7 @@ struct OuterSide {
   const void* v; long long ldv;
   const void* u;
   void* g;
-  int d;
+  int d, wide;
 };
 struct OuterArgs {
   OuterSide side[2];           // 0: dA [n][r][d], 1: dB [n][d][r]
@@ -543,9 +600,10 @@ struct OuterArgs {
 };
 
 template <int RT> constexpr int kOutQuads = kOutColWarps * 4 * RT * 32;
+template <int RT> constexpr int kOutSmem = 2 * kOutQuads<RT> * 16;
 
 template <int RT, bool DROP>
-__global__ void __launch_bounds__(kAdThreads, RT <= 4 ? 2 : 1)
+__global__ void __launch_bounds__(kAdThreads, RT <= 2 ? 2 : 1)
 adapter_outer_kernel(const OuterArgs p) {
   constexpr int kQuads = kOutQuads<RT>;
   extern __shared__ __align__(16) uint8_t smem[];
@@ -566,11 +624,10 @@ adapter_outer_kernel(const OuterArgs p) {
   } else if (a > 0) {
     t_hi = 0;
   }
-  const int c0 = slice * kOutCols + cw * 64;
-  const bf16* v = (const bf16*)sd.v;
-  const uint4* u = (const uint4*)sd.u;
-  const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
-  const bool drop = DROP && side == 0;
+  const int c0 = slice * kOutCols + cw * 64, c = c0 + 16 * q;
+  const bf16* v = (const bf16*)sd.v + c;
+  const uint4* u = (const uint4*)sd.u + lane;
+  const bool drop = DROP && side == 0, in0 = c < sd.d, in1 = c + 8 < sd.d;
   float acc[4][RT][4];
 #pragma unroll
   for (int i = 0; i < 4; ++i)
@@ -579,38 +636,50 @@ adapter_outer_kernel(const OuterArgs p) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) acc[i][rt][e] = 0.0f;
   const int step = (int)ctas * kOutRowWarps;
+  // rows of step t; -1: none (nothing is read, and the fragments of U hold zeros there)
+  auto rows_of = [&](int t, int (&row)[2]) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const long long pos = (long long)t * 16 + 8 * h + g;
+      row[h] = t >= t_hi ? -1 : p.tiles.row_adapter ? __ldcg(p.tiles.row_list + pos) : pos < p.n_rows ? (int)pos : -1;
+    }
+  };
+  struct Step { uint32_t x[2][8]; uint4 u[RT]; int row[2]; };
+  auto load = [&](int t, const int (&row)[2], Step& s) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      s.row[h] = row[h];
+      ld32<true>(v + (size_t)max(row[h], 0) * sd.ldv, sd.wide, row[h] >= 0 && in0, row[h] >= 0 && in1, s.x[h]);
+    }
+    if (t < t_hi)
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) s.u[rt] = ld_dep16(u + ((size_t)t * RT + rt) * 32);
+  };
   if (c0 < sd.d) {
+    int t = t_lo + (int)rank * kOutRowWarps + rw, ahead[2];
+    Step cur, nxt;
+    rows_of(t, ahead);
+    load(t, ahead, cur);
+    rows_of(t + step, ahead);
 #pragma unroll 1
-    for (int t = t_lo + (int)rank * kOutRowWarps + rw; t < t_hi; t += step) {
-      uint4 x[2][2];                                       // [rows g, g + 8][columns 8 q .., 32 + 8 q ..]
+    for (; t < t_hi; t += step) {
+      load(t + step, ahead, nxt);
+      rows_of(t + 2 * step, ahead);
+      if (drop)
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const long long pos = (long long)t * 16 + 8 * h + g;
-        const int row = p.tiles.row_adapter ? __ldcg(p.tiles.row_list + pos) : pos < p.n_rows ? (int)pos : -1;
+        for (int h = 0; h < 2; ++h) drop16(cur.x[h], p.drop, cur.row[h], c >> 3);
+      // columns become the MMA's rows: tile i has columns 16 (r / 2) + 4 i + r % 2 in its rows r = 0 .. 7, those + 2 in 8 .. 15
 #pragma unroll
-        for (int w = 0; w < 2; ++w) {
-          const int c = c0 + 32 * w + 8 * q;
-          x[h][w] = row >= 0 && c < sd.d ? ld_dep16(v + (size_t)row * sd.ldv + c) : zero;
-          if (drop) x[h][w] = drop8(x[h][w], drop_draws(p.drop, row, c >> 3), p.drop.thr16);
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t a0 = transpose8(cur.x[0][2 * i]), a1 = transpose8(cur.x[0][2 * i + 1]);
+        const uint32_t a2 = transpose8(cur.x[1][2 * i]), a3 = transpose8(cur.x[1][2 * i + 1]);
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+          mma_bf16_16816(acc[i][rt], a0, a1, a2, a3, cur.u[rt].z, cur.u[rt].w);
+          mma_bf16_16816(acc[i][rt], a0, a1, a2, a3, cur.u[rt].x, cur.u[rt].y);
         }
       }
-      uint4 uf[RT];
-#pragma unroll
-      for (int rt = 0; rt < RT; ++rt) uf[rt] = ld_dep16(u + ((size_t)t * RT + rt) * 32 + lane);
-      // columns become the MMA's rows: tile (w, j / 2) has columns 32 w + 8 (i / 2) + 2 j + i % 2 of its rows i
-#pragma unroll
-      for (int w = 0; w < 2; ++w)
-#pragma unroll
-        for (int jp = 0; jp < 2; ++jp) {
-          const uint32_t l0 = jp ? x[0][w].z : x[0][w].x, l1 = jp ? x[0][w].w : x[0][w].y;
-          const uint32_t h0 = jp ? x[1][w].z : x[1][w].x, h1 = jp ? x[1][w].w : x[1][w].y;
-          const uint32_t a0 = transpose8(l0), a1 = transpose8(l1), a2 = transpose8(h0), a3 = transpose8(h1);
-#pragma unroll
-          for (int rt = 0; rt < RT; ++rt) {
-            mma_bf16_16816(acc[2 * w + jp][rt], a0, a1, a2, a3, uf[rt].z, uf[rt].w);
-            mma_bf16_16816(acc[2 * w + jp][rt], a0, a1, a2, a3, uf[rt].x, uf[rt].y);
-          }
-        }
+      cur = nxt;
     }
   }
   auto quad = [&](int i, int rt) { return ((cw * 4 + i) * RT + rt) * 32 + lane; };
@@ -647,7 +716,7 @@ adapter_outer_kernel(const OuterArgs p) {
     const float val[2][2] = {{s.x, s.y}, {s.z, s.w}};
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const int c = slice * kOutCols + (mi >> 2) * 64 + ((mi >> 1) & 1) * 32 + 8 * (lg >> 1) + 2 * (2 * (mi & 1) + h) + (lg & 1);
+      const int c = slice * kOutCols + (mi >> 2) * 64 + 16 * (lg >> 1) + 2 * (2 * (mi & 3) + h) + (lg & 1);
       if (c >= sd.d) continue;
       if (side == 0) {
         out[(size_t)n0 * sd.d + c] = __float2bfloat16_rn(val[h][0]);
@@ -946,7 +1015,7 @@ inline int adapter_rank_tiles(int r) { return r <= 8 ? 1 : r <= 16 ? 2 : r <= 32
 
 // 16-row MMA tiles of a row tile.  Batches whose clusters find their tiles themselves take 16 rows: most of their
 // adapters have a row or two.
-inline int adapter_mt(int r, bool small) { return small ? 1 : adapter_rank_tiles(r) == 8 ? 2 : 4; }
+inline int adapter_mt(int, bool small) { return small ? 1 : 2; }
 inline bool adapter_small(const int32_t* row_adapter, int n_rows, bool backward) { return row_adapter && n_rows <= kAdSmallRows && !backward; }
 inline int adapter_tile_rows(bool bf, int r, bool small) { return bf ? 16 * adapter_mt(r, small) : kSimtM; }
 inline long long adapter_max_tiles(long long n_rows, int n, int m, bool one) {
@@ -974,13 +1043,14 @@ inline AdapterScratch adapter_scratch(bool bf, int n_rows, int n, int r, bool ba
   return s;
 }
 
+constexpr int kAdSmemPerSm = 220 * 1024;
 constexpr size_t kAdPlainSmem = 46 * 1024;    // dynamic shared memory that needs no attribute next to the kernels' static variables
 
-// Blocks of a cluster for `tiles` tiles that have rows: enough for two rounds of the SMs, no more than have a 32-wide block of either product for each warp,
-// and no more than shared memory for their sums allows.
-inline int adapter_ctas(long long tiles, int n_sms, int widest, int smem_limit_ctas) {
+// Blocks of a cluster for `tiles` tiles that have rows: enough for three blocks an SM, no more than have a `block` wide piece of
+// either product for each warp, and no more than shared memory for their sums allows.
+inline int adapter_ctas(long long tiles, int n_sms, int widest, int block, int smem_limit_ctas) {
   int c = 1;
-  while (c < 8 && tiles * c < 2 * n_sms && c * 2 * kAdWarps <= std::max(kAdWarps, (widest + 31) / 32) && c * 2 <= smem_limit_ctas) c *= 2;
+  while (c < 8 && tiles * c < 3 * n_sms && c * 2 * kAdWarps <= std::max(kAdWarps, (widest + block - 1) / block) && c * 2 <= smem_limit_ctas) c *= 2;
   return c;
 }
 
@@ -1007,9 +1077,10 @@ inline cudaError_t launch_cluster(bool dep, void (*kernel)(KP...), dim3 grid, di
 
 template <int MT, int RT, bool TRANS>
 inline cudaError_t launch_adapter_tile(const AdapterArgs<bf16>& a, long long tiles, long long live, int n_sms, bool dep, cudaStream_t st) {
-  const int room = std::max(1, (128 * 1024 - AdapterSmem<MT, RT>::bytes(0)) / AdapterSmem<MT, RT>::kRecv);
-  const int ctas = adapter_ctas(live, n_sms, std::max(a.d_k, a.d_n), room);
-  const size_t smem = AdapterSmem<MT, RT>::bytes(ctas);
+  using S = AdapterShape<MT, RT, TRANS>;
+  const int room = std::max(1, (kAdSmemPerSm / S::kMinBlocks - S::bytes(0)) / S::kRecv);
+  const int ctas = adapter_ctas(live, n_sms, std::max(a.d_k, a.d_n), 64, room);
+  const size_t smem = S::bytes(ctas);
   const dim3 grid((unsigned)(tiles * ctas)), cl(ctas);
   return a.drop.thr16 ? launch_cluster(dep, adapter_kernel<MT, RT, TRANS, true>, grid, cl, smem, st, a)
                       : launch_cluster(dep, adapter_kernel<MT, RT, TRANS, false>, grid, cl, smem, st, a);
@@ -1027,15 +1098,15 @@ inline cudaError_t launch_adapter(const AdapterArgs<bf16>& a, bool small, long l
       }
   }
   switch (rt) {
-    case 1: return launch_adapter_tile<4, 1, TRANS>(a, tiles, live, n_sms, dep, st);
-    case 2: return launch_adapter_tile<4, 2, TRANS>(a, tiles, live, n_sms, dep, st);
-    case 4: return launch_adapter_tile<4, 4, TRANS>(a, tiles, live, n_sms, dep, st);
+    case 1: return launch_adapter_tile<2, 1, TRANS>(a, tiles, live, n_sms, dep, st);
+    case 2: return launch_adapter_tile<2, 2, TRANS>(a, tiles, live, n_sms, dep, st);
+    case 4: return launch_adapter_tile<2, 4, TRANS>(a, tiles, live, n_sms, dep, st);
     default: return launch_adapter_tile<2, 8, TRANS>(a, tiles, live, n_sms, dep, st);
   }
 }
 template <bool TRANS>
 inline cudaError_t launch_adapter(const AdapterArgs<float>& a, bool, long long tiles, long long live, int n_sms, bool dep, cudaStream_t st) {
-  const int ctas = adapter_ctas(live, n_sms, std::max(a.d_k, a.d_n), 8);
+  const int ctas = adapter_ctas(live, n_sms, std::max(a.d_k, a.d_n), 32, 8);
   const size_t smem = AdapterSimtSmem::bytes(ctas);
   const dim3 grid((unsigned)(tiles * ctas)), cl(ctas);
   return a.drop.thr16 ? launch_cluster(dep, adapter_simt_kernel<TRANS, true>, grid, cl, smem, st, a)
@@ -1064,8 +1135,8 @@ template <int RT> inline cudaError_t launch_outer_rt(OuterArgs p, int n_sms, boo
   const int slices = p.slices0 + (p.side[1].d + kOutCols - 1) / kOutCols;
   const int ctas = outer_ctas((long long)slices * p.n, n_sms, (long long)p.n_rows / p.n / (16 * kOutRowWarps));
   const dim3 grid(slices, p.n, ctas), cl(1, 1, ctas);
-  return p.drop.thr16 ? launch_cluster(dep, adapter_outer_kernel<RT, true>, grid, cl, 2 * kOutQuads<RT> * 16, st, p)
-                      : launch_cluster(dep, adapter_outer_kernel<RT, false>, grid, cl, 2 * kOutQuads<RT> * 16, st, p);
+  return p.drop.thr16 ? launch_cluster(dep, adapter_outer_kernel<RT, true>, grid, cl, kOutSmem<RT>, st, p)
+                      : launch_cluster(dep, adapter_outer_kernel<RT, false>, grid, cl, kOutSmem<RT>, st, p);
 }
 inline cudaError_t launch_outer(bool bf, const OuterArgs& a, int n_sms, bool dep, cudaStream_t st) {
   if (bf) switch (adapter_rank_tiles(a.r)) {

@@ -1409,7 +1409,10 @@ int check_drop(const cmoe_dropout_config* d, int64_t rows, Drop* out) {
   if (d->row0 < 0 || d->row0 > (int64_t)4294967296LL - rows) return arg_fail(CMOE_ERR_INVALID_ARG, "dropout: row0 + rows exceeds 2^32");
   out->thr16 = thr << 16;
   out->inv = (float)(65536.0 / (65536.0 - thr));
-  out->k0 = (uint32_t)d->seed; out->k1 = (uint32_t)(d->seed >> 32);
+  for (uint32_t i = 0; i < 10; ++i) {
+    out->k[i][0] = (uint32_t)d->seed + i * 0x9E3779B9u;
+    out->k[i][1] = (uint32_t)(d->seed >> 32) + i * 0xBB67AE85u;
+  }
   out->off0 = (uint32_t)d->offset; out->off1 = (uint32_t)(d->offset >> 32);
   out->row0 = (uint32_t)d->row0;
   return CMOE_OK;
@@ -1433,6 +1436,9 @@ int check_rows_mat(const Mat& m, int64_t esz, const char* what) {
   }
   return CMOE_OK;
 }
+// Rows of bf16 that 32-byte accesses may walk.
+bool wide_rows(const Mat& m, int64_t width) { return !m.p || (((uintptr_t)m.p & 31) == 0 && m.ld % 16 == 0 && width % 16 == 0); }
+
 #define RC_TRY(expr)                      \
   do {                                    \
     const int rc_ = (expr);               \
@@ -1489,6 +1495,8 @@ int adapter_forward_launch(const cmoe_adapters* ad, AdapterPass<T>& p, const Mat
   p.a.base = (const T*)base.p; p.a.ld_base = base.ld;
   p.a.out = (T*)out.p; p.a.ld_out = out.ld;
   p.a.z_out = z; p.a.d_k = ad->d_in; p.a.d_n = ad->d_out; p.a.drop = drop;
+  p.a.wide_x = wide_rows(x, ad->d_in) && wide_rows({ad->a, ad->d_in, ad->d_in}, ad->d_in);
+  p.a.wide_n = wide_rows(base, ad->d_out) && wide_rows(out, ad->d_out);
   if (p.plan.row_list) CU_TRY(launch_adapter_plan(p.a, p.m, p.plan, st));
   CU_TRY((launch_adapter<false>(p.a, p.small, p.tiles, p.live, n_sms, p.plan.row_list != nullptr, st)));
   return CMOE_OK;
@@ -1529,13 +1537,15 @@ int adapter_backward_impl(const cmoe_adapters* ad, const Mat& dy, const Mat& x, 
   p.a.base = (const T*)dx_base.p; p.a.ld_base = dx_base.ld;
   p.a.out = (T*)dx.p; p.a.ld_out = dx.ld;
   p.a.z_in = z; p.a.d_k = ad->d_out; p.a.d_n = ad->d_in; p.a.drop = drop;
+  p.a.wide_x = wide_rows(dy, ad->d_out);
+  p.a.wide_n = wide_rows(dx_base, ad->d_in) && wide_rows(dx, ad->d_in);
   if (!grad_a) p.a.u_e = p.a.u_z = nullptr;
   if (p.plan.row_list) CU_TRY(launch_adapter_plan(p.a, p.m, p.plan, st));
   CU_TRY((launch_adapter<true>(p.a, false, p.tiles, p.live, n_sms, p.plan.row_list != nullptr, st)));
   if (!grad_a) return CMOE_OK;
   OuterArgs o{};
-  o.side[0] = {x.p, x.ld, p.a.u_e, grad_a, ad->d_in};
-  o.side[1] = {dy.p, dy.ld, p.a.u_z, grad_b, ad->d_out};
+  o.side[0] = {x.p, x.ld, p.a.u_e, grad_a, ad->d_in, wide_rows(x, ad->d_in)};
+  o.side[1] = {dy.p, dy.ld, p.a.u_z, grad_b, ad->d_out, p.a.wide_x};
   o.n_rows = n_rows; o.n = ad->n_adapters; o.r = ad->rank; o.m = p.m; o.tiles = p.a.tiles; o.drop = drop;
   CU_TRY(launch_outer(sizeof(T) == 2, o, n_sms, true, st));
   return CMOE_OK;

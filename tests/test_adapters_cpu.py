@@ -163,9 +163,9 @@ def test_capacity_refusals(lib):
 
 @pytest.mark.parametrize("bf", [0, 1])
 def test_scratch_holds_the_worst_case(lib, bf):
-    """Tiles of 64 or 32 rows: every adapter and the rows without one may leave a tile part filled."""
+    """Tiles of at least 32 rows: every adapter and the rows without one may leave a tile part filled."""
     for rows, n, r in itertools.product((1, 31, 257, 5000), (1, 7, 1024), (8, 16, 32, 64)):
-        m = 32 if bf or r > 32 else 64
+        m = 32
         groups = min(n + 1, rows)
         tiles = max((rows - groups + 1 + m - 1) // m + groups - 1, 1)            # one large group, the others a row each
         ad = _ad(n_adapters=n, rank=r, dtype=bf)
