@@ -428,8 +428,8 @@ int64_t cmoe_adapter_scratch_bytes(const cmoe_adapters* ad, int32_t n_rows, int3
  * [0, n_adapters) means no adapter: out_t = base_t.  xd is x, or its dropout by `drop` (NULL: none).
  *   x    : device, [n_rows, d_in], row stride ldx;  base : device, [n_rows, d_out], row stride ld_base, or NULL (zero): what the
  *          shared projection gave for the rows;  out : device, [n_rows, d_out], row stride ld_out; may be base (same pointer
- *          and stride), overlaps neither x nor base otherwise.  Strides in elements, at least the width; pointers and strides
- *          are multiples of 16 bytes.  Rows of other matrices may lie between (column slices of a wider one).
+ *          and stride), overlaps neither x nor base otherwise.  Strides in elements, at least the width, at most 2^28; pointers and
+ *          strides are multiples of 16 bytes.  Rows of other matrices may lie between (column slices of a wider one).
  *   row_adapter : device int32 [n_rows], in any order, or NULL: every row takes adapter 0.
  *   z    : device float [n_rows, rank] or NULL; receives A_a xd_t (zeros for rows without an adapter), for the backward pass.
  *   scratch : needed where row_adapter is given and n_rows > 256.
@@ -454,6 +454,11 @@ int cmoe_adapter_backward(const cmoe_adapters* ad, const void* dy, int64_t ld_dy
                           const int32_t* row_adapter, int32_t n_rows, const cmoe_dropout_config* drop, const void* dx_base,
                           int64_t ld_dx_base, void* dx, int64_t ld_dx, void* grad_a, void* grad_b, void* scratch,
                           int64_t scratch_bytes, void* stream);
+
+/* Device-side error word of this device's cmoe_adapter_backward calls: 0, or a code written by a kernel whose bounded wait for
+ * a copy ran out (the gradients of that call are undefined).  Synchronises `stream`.  Returns CMOE_ERR_DEVICE_TIMEOUT when the
+ * word is non-zero; it is reported once and cleared.  device_error_word may be NULL.  Errors: CUDA. */
+int cmoe_adapter_status(int32_t* device_error_word, void* stream);
 
 /* out_t = F_MoE(x_t) + s_a B_a A_a x_t: cmoe_ffn_forward with an adapter per request beside the layer, which all of them share.
  * The adapters' d_in and d_out are the layer's d_model and their dtype is the layer's; x, T, out as in cmoe_ffn_forward,

@@ -27,7 +27,8 @@ EXPORTS = [
     "cmoe_layer_launch_count", "cmoe_layer_gemm_forms", "cmoe_layer_enable_stage_timing", "cmoe_layer_stage_times",
     "cmoe_layer_destroy", "cmoe_token_permute_scratch_bytes",
     "cmoe_token_permute", "cmoe_token_permute_static", "cmoe_status_string", "cmoe_last_error",
-    "cmoe_dropout", "cmoe_adapter_scratch_bytes", "cmoe_adapter_forward", "cmoe_adapter_backward", "cmoe_ffn_forward_adapted",
+    "cmoe_dropout", "cmoe_adapter_scratch_bytes", "cmoe_adapter_forward", "cmoe_adapter_backward", "cmoe_adapter_status",
+    "cmoe_ffn_forward_adapted",
 ]
 
 
@@ -100,6 +101,7 @@ def load() -> C.CDLL:
     lib.cmoe_adapter_scratch_bytes.restype = i64
     lib.cmoe_adapter_forward.argtypes = [vp, vp, i64, vp, i32, vp, vp, i64, vp, i64, vp, vp, i64, vp]
     lib.cmoe_adapter_backward.argtypes = [vp, vp, i64, vp, i64, vp, vp, i32, vp, vp, i64, vp, i64, vp, vp, vp, i64, vp]
+    lib.cmoe_adapter_status.argtypes = [C.POINTER(i32), vp]
     lib.cmoe_ffn_forward_adapted.argtypes = [vp, vp, i32, vp, vp, vp, vp, i64, vp]
     lib.cmoe_status_string.argtypes = [C.c_int]
     lib.cmoe_status_string.restype = C.c_char_p
@@ -205,7 +207,7 @@ class Layer:
             with elsewhere:
                 return self.forward_adapted(x, a, b, row_adapter, scale, out, scratch)
         ad = _adapters(dtype, dev, a, b, scale)
-        ids = _adapter_ids(row_adapter, rows, dev)
+        ids = None if row_adapter is None else _like(row_adapter, "row_adapter", (rows,), _torch.int32, dev)
         if out is None:
             out = x.new_empty((rows, d))
         if d != self.d_model or ldx != d or _matrix(out, "out", rows, d, dtype, dev) != d:
@@ -456,6 +458,17 @@ def _drop_config(drop: Optional[Dropout]):
     return None if drop is None else CmoeDropoutConfig(drop.p, drop.seed & 0xFFFFFFFFFFFFFFFF, drop.offset & 0xFFFFFFFFFFFFFFFF, drop.row0)
 
 
+_torch = None      # the module, once the first of the calls below has imported it
+
+
+def _need_torch():
+    global _torch
+    if _torch is None:
+        import torch
+        _torch = torch
+    return _torch
+
+
 def _matrix(t, what: str, rows: int, cols: int, dtype, dev: int) -> int:
     """The row stride of a row-strided [rows, cols] matrix of this type and device."""
     stride = t.stride()
@@ -470,7 +483,8 @@ def _rows(t, what: str):
     if dev < 0 or t.dim() != 2:
         raise ValueError(f"{what}: a two-dimensional CUDA tensor is expected")
     rows, cols = t.shape
-    return rows, cols, _matrix(t, what, rows, cols, t.dtype, dev), t.dtype, dev
+    dtype = t.dtype
+    return rows, cols, _matrix(t, what, rows, cols, dtype, dev), dtype, dev
 
 
 def _like(t, what: str, shape, dtype, dev: int) -> int:
@@ -483,17 +497,21 @@ def _like(t, what: str, shape, dtype, dev: int) -> int:
 def _elsewhere(dev: int, stream):
     """None where the call's device is current and its work goes to that device's current stream, else a context in which
     that holds: what the call allocates and frees then belongs to the stream that uses it."""
-    import torch
+    torch = _torch or _need_torch()
     if stream is not None:
         if stream.device.index != dev:
             raise ValueError("the stream and the tensors are on different devices")
         return torch.cuda.stream(stream)
-    return None if torch.cuda.current_device() == dev else torch.cuda.device(dev)
+    return None if torch._C._cuda_getDevice() == dev else torch.cuda.device(dev)
 
 
 def _current_stream(dev: int) -> int:
-    import torch
-    return torch._C._cuda_getCurrentRawStream(dev)             # torch.cuda.current_stream(dev).cuda_stream, without the objects
+    return _torch._C._cuda_getCurrentRawStream(dev)            # torch.cuda.current_stream(dev).cuda_stream, without the objects
+
+
+def _new_rows(like, rows: int, cols: int, ld: int):
+    """An uninitialised contiguous matrix of the type and device of `like`, whose row stride is ld."""
+    return _torch.empty_like(like) if ld == cols and like.shape[1] == cols else like.new_empty((rows, cols))
 
 
 def dropout(x, drop: Dropout, residual=None, out=None, stream=None):
@@ -505,12 +523,13 @@ def dropout(x, drop: Dropout, residual=None, out=None, stream=None):
         with elsewhere:
             return dropout(x, drop, residual, out)
     code = _dtype_code(x)
-    ld_res = 0 if residual is None else _matrix(residual, "residual", rows, cols, dtype, dev)
+    ld_res, res_ptr = (0, None) if residual is None else (_matrix(residual, "residual", rows, cols, dtype, dev), residual.data_ptr())
     if out is None:
-        out = x.new_empty((rows, cols))
-    ld_out = _matrix(out, "out", rows, cols, dtype, dev)
-    st = load().cmoe_dropout(x.data_ptr(), ldx, None if residual is None else residual.data_ptr(), ld_res, rows, cols, code,
-                             C.byref(_drop_config(drop)), out.data_ptr(), ld_out, _current_stream(dev))
+        out, ld_out = _new_rows(x, rows, cols, ldx), cols
+    else:
+        ld_out = _matrix(out, "out", rows, cols, dtype, dev)
+    st = load().cmoe_dropout(x.data_ptr(), ldx, res_ptr, ld_res, rows, cols, code, C.byref(_drop_config(drop)), out.data_ptr(), ld_out,
+                             _current_stream(dev))
     if st:
         _check(st, "cmoe_dropout")
     return out
@@ -519,19 +538,11 @@ def dropout(x, drop: Dropout, residual=None, out=None, stream=None):
 def _adapters(dtype, dev: int, a, b, scale) -> CmoeAdapters:
     n, r, d_in = a.shape
     d_out = b.shape[1]
-    import torch
-    code = CMOE_BF16 if dtype is torch.bfloat16 else CMOE_FP32 if dtype is torch.float32 else None
+    code = CMOE_BF16 if dtype is _torch.bfloat16 else CMOE_FP32 if dtype is _torch.float32 else None
     if code is None:
         raise TypeError(f"unsupported dtype {dtype}")
     return CmoeAdapters(n, r, d_in, d_out, code, _like(a, "a", (n, r, d_in), dtype, dev), _like(b, "b", (n, d_out, r), dtype, dev),
-                        None if scale is None else _like(scale, "scale", (n,), torch.float32, dev))
-
-
-def _adapter_ids(row_adapter, rows: int, dev: int):
-    if row_adapter is None:
-        return None
-    import torch
-    return _like(row_adapter, "row_adapter", (rows,), torch.int32, dev)
+                        None if scale is None else _like(scale, "scale", (n,), _torch.float32, dev))
 
 
 ADAPTER_SMALL_ROWS = 256     # row counts up to which cmoe_adapter_forward needs no scratch
@@ -542,13 +553,11 @@ def _adapter_scratch(ad: CmoeAdapters, rows: int, ids, backward: int, scratch, l
     if scratch is None:
         if not backward and (ids is None or rows <= ADAPTER_SMALL_ROWS):
             return None, None, 0
-        import torch
         nbytes = load().cmoe_adapter_scratch_bytes(C.byref(ad), rows, 0 if ids is None else 1, backward)
-        scratch = like.new_empty((nbytes,), dtype=torch.uint8)
+        scratch = like.new_empty((nbytes,), dtype=_torch.uint8)
         return scratch, scratch.data_ptr(), nbytes
-    import torch
     n = scratch.numel()
-    return scratch, _like(scratch, "scratch", (n,), torch.uint8, like.get_device()), n
+    return scratch, _like(scratch, "scratch", (n,), _torch.uint8, like.get_device()), n
 
 
 def adapter_forward(x, a, b, row_adapter=None, scale=None, base=None, dropout: Optional[Dropout] = None, want_z: bool = False,
@@ -562,23 +571,23 @@ def adapter_forward(x, a, b, row_adapter=None, scale=None, base=None, dropout: O
     if elsewhere is not None:
         with elsewhere:
             return adapter_forward(x, a, b, row_adapter, scale, base, dropout, want_z, out, z, scratch)
-    import torch
     ad = _adapters(dtype, dev, a, b, scale)
     if d_in != ad.d_in:
         raise ValueError(f"x: expected rows of {ad.d_in}")
-    d_out = ad.d_out
-    ld_base = 0 if base is None else _matrix(base, "base", rows, d_out, dtype, dev)
-    ids = _adapter_ids(row_adapter, rows, dev)
+    d_out, ld_base, base_ptr = ad.d_out, 0, None
+    if base is not None:
+        ld_base, base_ptr = _matrix(base, "base", rows, d_out, dtype, dev), base.data_ptr()
+    ids = None if row_adapter is None else _like(row_adapter, "row_adapter", (rows,), _torch.int32, dev)
     if out is None:
-        out = x.new_empty((rows, d_out))
-    ld_out = _matrix(out, "out", rows, d_out, dtype, dev)
+        out, ld_out = _new_rows(x if base is None else base, rows, d_out, ldx if base is None else ld_base), d_out
+    else:
+        ld_out = _matrix(out, "out", rows, d_out, dtype, dev)
     if z is None and want_z:
-        z = x.new_empty((rows, ad.rank), dtype=torch.float32)
-    z_ptr = None if z is None else _like(z, "z", (rows, ad.rank), torch.float32, dev)
+        z = x.new_empty((rows, ad.rank), dtype=_torch.float32)
+    z_ptr = None if z is None else _like(z, "z", (rows, ad.rank), _torch.float32, dev)
     scratch, s_ptr, s_bytes = _adapter_scratch(ad, rows, ids, 0, scratch, x)
     st = load().cmoe_adapter_forward(C.byref(ad), x.data_ptr(), ldx, ids, rows, None if dropout is None else C.byref(_drop_config(dropout)),
-                                     None if base is None else base.data_ptr(), ld_base, out.data_ptr(), ld_out, z_ptr,
-                                     s_ptr, s_bytes, _current_stream(dev))
+                                     base_ptr, ld_base, out.data_ptr(), ld_out, z_ptr, s_ptr, s_bytes, _current_stream(dev))
     if st:
         _check(st, "cmoe_adapter_forward")
     return out if z is None else (out, z)
@@ -593,33 +602,40 @@ def adapter_backward(dy, x, z, a, b, row_adapter=None, scale=None, dx_base=None,
     if elsewhere is not None:
         with elsewhere:
             return adapter_backward(dy, x, z, a, b, row_adapter, scale, dx_base, dropout, want_dx, want_grads, dx, grad_a, grad_b, scratch)
-    import torch
     ad = _adapters(dtype, dev, a, b, scale)
     if d_out != ad.d_out:
         raise ValueError(f"dy: expected rows of {ad.d_out}")
     d_in = ad.d_in
-    ids = _adapter_ids(row_adapter, rows, dev)
+    ids = None if row_adapter is None else _like(row_adapter, "row_adapter", (rows,), _torch.int32, dev)
     ldx = ld_base = ld_dx = 0
-    x_ptr = z_ptr = dx_ptr = ga_ptr = gb_ptr = None
+    x_ptr = z_ptr = dx_ptr = ga_ptr = gb_ptr = base_ptr = None
+    if dx_base is not None:
+        ld_base, base_ptr = _matrix(dx_base, "dx_base", rows, d_in, dtype, dev), dx_base.data_ptr()
     if want_dx or dx is not None:
         if dx is None:
             dx = dy.new_empty((rows, d_in))
         ld_dx, dx_ptr = _matrix(dx, "dx", rows, d_in, dtype, dev), dx.data_ptr()
-    if dx_base is not None:
-        ld_base = _matrix(dx_base, "dx_base", rows, d_in, dtype, dev)
     if want_grads or grad_a is not None or grad_b is not None:
-        ldx, x_ptr, z_ptr = _matrix(x, "x", rows, d_in, dtype, dev), x.data_ptr(), _like(z, "z", (rows, ad.rank), torch.float32, dev)
-        grad_a = torch.empty_like(a) if grad_a is None else grad_a
-        grad_b = torch.empty_like(b) if grad_b is None else grad_b
+        ldx, x_ptr, z_ptr = _matrix(x, "x", rows, d_in, dtype, dev), x.data_ptr(), _like(z, "z", (rows, ad.rank), _torch.float32, dev)
+        grad_a = _torch.empty_like(a) if grad_a is None else grad_a
+        grad_b = _torch.empty_like(b) if grad_b is None else grad_b
         ga_ptr, gb_ptr = _like(grad_a, "grad_a", a.shape, dtype, dev), _like(grad_b, "grad_b", b.shape, dtype, dev)
     scratch, s_ptr, s_bytes = _adapter_scratch(ad, rows, ids, 1, scratch, dy)
     st = load().cmoe_adapter_backward(C.byref(ad), dy.data_ptr(), ld_dy, x_ptr, ldx, z_ptr, ids, rows,
-                                      None if dropout is None else C.byref(_drop_config(dropout)),
-                                      None if dx_base is None else dx_base.data_ptr(), ld_base, dx_ptr, ld_dx, ga_ptr, gb_ptr,
-                                      s_ptr, s_bytes, _current_stream(dev))
+                                      None if dropout is None else C.byref(_drop_config(dropout)), base_ptr, ld_base, dx_ptr, ld_dx,
+                                      ga_ptr, gb_ptr, s_ptr, s_bytes, _current_stream(dev))
     if st:
         _check(st, "cmoe_adapter_backward")
     return dx, grad_a, grad_b
+
+
+def adapter_status(stream=None) -> int:
+    """cmoe_adapter_status: the current device's error word of the adapters' backward calls (0: none), reported once."""
+    w = C.c_int32()
+    st = load().cmoe_adapter_status(C.byref(w), _stream_ptr(stream))
+    if st not in (0, -6):
+        _check(st, "cmoe_adapter_status")
+    return w.value
 
 
 def adapter_scratch_bytes(n_adapters: int, rank: int, d_in: int, d_out: int, dtype, n_rows: int, with_row_adapter: bool = True,

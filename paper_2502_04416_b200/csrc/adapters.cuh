@@ -19,6 +19,7 @@
 #include "permute.cuh"
 #include "router_cluster.cuh"
 #include "router_mma.cuh"
+#include "umma_gemm.cuh"
 
 namespace cmoe {
 
@@ -62,20 +63,21 @@ adapter_plan_kernel(const int32_t* row_adapter, int n_rows, int n, int m, const 
   __syncthreads();
   int32_t* mine = hist + warp * groups;
   // the groups of 32 kBatch rows from r0 on, their loads in flight at once (-1 behind the warp's last row)
-  constexpr int kBatch = 8;
-  auto groups_of = [&](long long r0, int (&v)[kBatch]) {
+  constexpr int kBatch = 16;
+  int v[kBatch];
+  auto groups_of = [&](long long r0) {
 #pragma unroll
     for (int i = 0; i < kBatch; ++i) {
       const long long row = r0 + 32 * i + lane;
-      v[i] = row < hi ? __ldcg(row_adapter + row) : 0;
-      v[i] = row < hi ? ((unsigned)v[i] < (unsigned)n ? v[i] : n) : -1;
+      v[i] = row < hi ? __ldcg(row_adapter + row) : -1;
+      if (row < hi && (unsigned)v[i] >= (unsigned)n) v[i] = n;
     }
   };
   for (long long r0 = lo; r0 < hi; r0 += 32 * kBatch) {
-    int v[kBatch];
-    groups_of(r0, v);
+    groups_of(r0);
 #pragma unroll
     for (int i = 0; i < kBatch; ++i) {
+      if (r0 + 32 * i >= hi) break;
       const unsigned same = __match_any_sync(0xffffffffu, v[i]);
       if (v[i] >= 0 && (same & lt) == 0) mine[v[i]] += __popc(same);
       __syncwarp();
@@ -84,28 +86,19 @@ adapter_plan_kernel(const int32_t* row_adapter, int n_rows, int n, int m, const 
   __syncthreads();
   for (int g = threadIdx.x; g < groups; g += blockDim.x) {
     int run = 0;
-    for (int w = 0; w < 32; ++w) { const int v = hist[w * groups + g]; hist[w * groups + g] = run; run += v; }
+#pragma unroll 8
+    for (int w = 0; w < 32; ++w) { const int c = hist[w * groups + g]; hist[w * groups + g] = run; run += c; }
     count[g] = run;
     tiles[g] = (run + m - 1) / m;
   }
   __syncthreads();
   block_scan_groups(tiles, start, groups, sums);
   for (int g = threadIdx.x; g <= groups; g += blockDim.x) o.tile_start[g] = start[g];
-  const int n_tiles = start[groups];
-  for (int t = threadIdx.x; t < n_tiles; t += blockDim.x) {
-    int a = 0, b = groups;                   // start[a] <= t < start[b]
-    while (b - a > 1) {
-      const int c = (a + b) >> 1;
-      if (start[c] <= t) a = c; else b = c;
-    }
-    o.tile_adapter[t] = a;
-    for (int i = max(0, count[a] - (t - start[a]) * m); i < m; ++i) o.row_list[(size_t)t * m + i] = -1;
-  }
   for (long long r0 = lo; r0 < hi; r0 += 32 * kBatch) {
-    int v[kBatch];
-    groups_of(r0, v);
+    if (hi - lo > 32 * kBatch) groups_of(r0);            // a warp's only batch is still there
 #pragma unroll
     for (int i = 0; i < kBatch; ++i) {
+      if (r0 + 32 * i >= hi) break;
       const int g = v[i];
       const unsigned same = __match_any_sync(0xffffffffu, g);
       const int before = g >= 0 ? mine[g] : 0;
@@ -116,6 +109,16 @@ adapter_plan_kernel(const int32_t* row_adapter, int n_rows, int n, int m, const 
       }
       __syncwarp();
     }
+  }
+  const int n_tiles = start[groups];
+  for (int t = threadIdx.x; t < n_tiles; t += blockDim.x) {
+    int a = 0, b = groups;                               // start[a] <= t < start[b]
+    while (b - a > 1) {
+      const int c = (a + b) >> 1;
+      if (start[c] <= t) a = c; else b = c;
+    }
+    o.tile_adapter[t] = a;
+    for (int i = max(0, count[a] - (t - start[a]) * m); i < m; ++i) o.row_list[(size_t)t * m + i] = -1;
   }
 }
 inline size_t adapter_plan_smem(int n) { return (size_t)(35 * (n + 1) + 1 + 32) * sizeof(int32_t); }
@@ -138,32 +141,44 @@ __device__ __forceinline__ int adapter_tile(const AdTiles& t, int n_rows, int n,
     __syncthreads();
     return __ldcg(t.tile_adapter + tile);
   }
-  // tile: the row that may head a tile.  It does if a multiple of M rows with its adapter come before it.
-  __shared__ uint32_t words[kAdSmallRows / 32];
-  __shared__ int32_t head;
+  // A row heads a tile if a multiple of M rows with its adapter come before it; tile t belongs to the t-th such row.
+  static_assert(kAdSmallRows == kAdThreads, "one thread a row");
+  __shared__ __align__(16) int32_t ids[kAdSmallRows];
+  __shared__ uint32_t heads[kAdWarps];
+  __shared__ int2 head;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t lt = (1u << lane) - 1u;
   int a = -2;
   if ((int)threadIdx.x < n_rows) {
     a = __ldcg(t.row_adapter + threadIdx.x);
     a = (unsigned)a < (unsigned)n ? a : n;
   }
-  if ((int)threadIdx.x == tile) head = a;
+  ids[threadIdx.x] = a;
   for (int i = threadIdx.x; i < M; i += kAdThreads) rows[i] = -1;
   __syncthreads();
-  const int mine = head;
-  const uint32_t vote = __ballot_sync(0xffffffffu, a == mine);
-  if (lane == 0) words[warp] = vote;
+  int rank = __popc(__match_any_sync(0xffffffffu, a) & lt);
+  if (a >= 0)
+    for (int i = 0; i < 32 * warp; i += 4) {
+      const int4 v = *reinterpret_cast<const int4*>(ids + i);
+      rank += (v.x == a) + (v.y == a) + (v.z == a) + (v.w == a);
+    }
+  const bool is_head = a >= 0 && rank % M == 0;
+  const uint32_t vote = __ballot_sync(0xffffffffu, is_head);
+  if (lane == 0) heads[warp] = vote;
   __syncthreads();
-  int rank = __popc(vote & ((1u << lane) - 1u)), first = 0;
-  for (int w = 0; w < kAdSmallRows / 32; ++w) {
-    if (w < warp) rank += __popc(words[w]);
-    if (w < (tile >> 5)) first += __popc(words[w]);
+  int at = __popc(vote & lt), n_heads = 0;
+  for (int w = 0; w < kAdWarps; ++w) {
+    const int c = __popc(heads[w]);
+    if (w < warp) at += c;
+    n_heads += c;
   }
-  first += __popc(words[tile >> 5] & ((1u << (tile & 31)) - 1u));
-  if (first % M != 0) return -1;
-  if (a == mine && rank >= first && rank < first + M) rows[rank - first] = threadIdx.x;
+  if (tile >= n_heads) return -1;
+  if (is_head && at == tile) head = make_int2(a, rank);
   __syncthreads();
-  return mine;
+  const int2 h = head;
+  if (a == h.x && rank >= h.y && rank < h.y + M) rows[rank - h.y] = threadIdx.x;
+  __syncthreads();
+  return h.x;
 }
 
 // ---------------------------------------------------------------------------------------------------------------------
@@ -241,40 +256,46 @@ __device__ __forceinline__ void adapter_none(const AdapterArgs<T>& p, const int3
 }
 
 // ---- bf16 -------------------------------------------------------------------------------------------------------------
-// MT: 16-row MMA tiles of a row tile; RT: 8-wide tiles of the rank (padded with zeros); TRANS: backward.
+// MT: 16-row MMA tiles of a row tile; RT: 8-wide tiles of the rank (padded); TRANS: backward.
 //
 // A lane of an 8 x 4 fragment loads 32 neighbouring bytes of its row: four lanes make whole 128-byte lines, and 32 bytes are
 // the operands of four k steps (k inside a 64-wide block is permuted alike on both sides, which leaves the sums as they are)
 // or eight tiles' results of one lane.  Loads that are 16 bytes wide, or go by way of shared memory, are bound by L1 instead of
 // HBM (16384 rows x 4096, rank 16, rows in and out: 106 us through a ring of asynchronous copies, L1 76 % busy).  What is in
-// flight is left to the number of resident warps.  At ranks above 32 two warps share the rows and split the rank.
+// flight is left to the number of resident warps and the tile's height.  At ranks above 16 the warps that share rows split the
+// rank, 16 each.  Loads past the end of a row, a column or the rank read the last valid place instead: what they bring meets
+// zeros in the other operand, or is not stored.
 template <int MT, int RT, bool TRANS> struct AdapterShape {
   static constexpr int kM = 16 * MT, kR = 8 * RT;
-  static constexpr int kSplit = RT == 8 ? 2 : 1, kRtw = RT / kSplit, kGroups = kAdWarps / kSplit;   // warps of a rank's share
+  static constexpr int kSplit = RT <= 2 ? 1 : RT / 2, kRtw = RT / kSplit, kGroups = kAdWarps / kSplit;   // warps of a rank's share
   static constexpr int kQuads = MT * RT * 32;
   // elements between the middle's rows: no two of a fragment's lanes meet in a bank
   static constexpr int kStride = TRANS ? (RT == 1 ? 8 : kR + 8) : RT == 8 ? 96 : kR;
   static constexpr int kPart = kGroups / 2 * kQuads * 16, kRecv = kQuads * 16, kMid = 2 * kM * kStride * 2;
   static constexpr int bytes(int ctas) { return kPart + ctas * kRecv + kMid + kM * 4; }
-  static constexpr int kMinBlocks = MT == 1 ? (RT <= 2 ? 3 : 2) : RT == 8 ? 1 : 2;
+  static constexpr int kMinBlocks = MT == 1 && RT <= 2 ? 3 : 2;
 };
 
-// 32 bytes in two halves; zeros where a half is not wanted.  wide: the row starts on a 32-byte boundary and both halves go together.
+// 32 bytes: columns c .. c + 15 of a row of `width`; past its end, the last ones again.  wide: the row starts on a 32-byte
+// boundary and is made of whole 32-byte pieces.
 template <bool STREAM>
-__device__ __forceinline__ void ld32(const bf16* p, bool wide, bool in0, bool in1, uint32_t (&r)[8]) {
+__device__ __forceinline__ void ld32(const bf16* row, int c, int width, bool wide, uint32_t (&r)[8]) {
   if (wide) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) r[i] = 0u;
-    if (in0) {
-      if (STREAM) ld256_stream(p, r);
-      else
-        asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-                     : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "l"(p) : "memory");
-    }
+    const bf16* p = row + min(c, width - 16);
+    if (STREAM) ld256_stream(p, r);
+    else
+      asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                   : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "l"(p) : "memory");
   } else {
-    const uint4 zero = make_uint4(0u, 0u, 0u, 0u), a = in0 ? ld_dep16(p) : zero, b = in1 ? ld_dep16(p + 8) : zero;
+    const uint4 a = ld_dep16(row + min(c, width - 8)), b = ld_dep16(row + min(c + 8, width - 8));
     r[0] = a.x; r[1] = a.y; r[2] = a.z; r[3] = a.w; r[4] = b.x; r[5] = b.y; r[6] = b.z; r[7] = b.w;
   }
+}
+// Zeros in what of those columns lies past the end.
+__device__ __forceinline__ void clear_tail(uint32_t (&r)[8], int c, int width) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    if (c + (i < 4 ? 0 : 8) >= width) r[i] = 0u;
 }
 __device__ __forceinline__ void drop16(uint32_t (&r)[8], const Drop& d, uint32_t row, uint32_t block) {
 #pragma unroll
@@ -285,6 +306,13 @@ __device__ __forceinline__ void drop16(uint32_t (&r)[8], const Drop& d, uint32_t
     r[4 * h + 2] = drop_pair(r[4 * h + 2], w.z, d.thr16);
     r[4 * h + 3] = drop_pair(r[4 * h + 3], w.w, d.thr16);
   }
+}
+// Asks for `bytes` bytes from p on in L2; both are multiples of 16.
+__device__ __forceinline__ void prefetch_l2(const void* p, int bytes) {
+  asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(p), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ const bf16* row_at(const bf16* m, uint32_t row, uint32_t pitch) {
+  return reinterpret_cast<const bf16*>(reinterpret_cast<const char*>(m) + (uint64_t)row * pitch);
 }
 
 template <int MT, int RT, bool TRANS, bool DROP>
@@ -309,7 +337,7 @@ adapter_kernel(const AdapterArgs<bf16> p) {
     return;
   }
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
-  int row_of[MT][2];
+  uint32_t row_of[MT][2];
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
@@ -317,9 +345,37 @@ adapter_kernel(const AdapterArgs<bf16> p) {
       const int row = rows[mt * 16 + 8 * h + g];
       row_of[mt][h] = row < 0 ? rows[0] : row;           // a row's sums are its own: rows past the end repeat the first
     }
+  const uint32_t x_pitch = (uint32_t)p.ldx * 2, base_pitch = (uint32_t)p.ld_base * 2, out_pitch = (uint32_t)p.ld_out * 2;
+  const bf16* w2 = p.w2 + (size_t)a * p.r * p.d_n;
+  const int nb0 = (int)rank * kAdWarps + warp, n_cols = p.out ? p.d_n : 0;
+  const int kg = warp / S::kSplit, rt0 = (warp % S::kSplit) * kRtw;
+  const bf16* w1 = p.w1 + (size_t)a * p.r * p.d_k;
+  if (MT == 1) {
+    // Few rows: what each warp will read comes from HBM, and all of it is asked for now, in L2: blocks of [width][r] weights as
+    // they lie, the other weights' and the rows' 128-byte lines one a lane.
+    const auto line = [](const bf16* row, int c, int width) {
+      if (c < width) asm volatile("prefetch.global.L2 [%0];" ::"l"(row + c));
+    };
+    const int my_row = rows[lane & 15];
+    for (int kb = (int)rank * kGroups + kg; kb * 64 < p.d_k; kb += (int)ctas * kGroups) {
+      const int c = kb * 64;
+      if (TRANS && lane == 0) prefetch_l2(w1 + (size_t)c * p.r, min(64, p.d_k - c) * p.r * 2);
+      if (lane < 16) {
+        if (my_row >= 0) line(row_at(p.x, my_row, x_pitch), c, p.d_k);
+      } else if (!TRANS && rt0 * 8 + lane - 16 < p.r) {
+        line(w1 + (size_t)(rt0 * 8 + lane - 16) * p.d_k, c, p.d_k);
+      }
+    }
+    for (int nb = nb0; nb * 64 < n_cols; nb += (int)ctas * kAdWarps) {
+      const int c = nb * 64;
+      if (!TRANS && lane == 0) prefetch_l2(w2 + (size_t)c * p.r, min(64, n_cols - c) * p.r * 2);
+      if (p.base && lane < 16 && my_row >= 0) line(row_at(p.base, my_row, base_pitch), c, n_cols);
+      if (TRANS)
+        for (int n = lane; n < p.r; n += 32) line(w2 + (size_t)n * p.d_n, c, n_cols);
+    }
+  }
 
   // ---- first product: [M, d_k] x [d_k, r], 64-wide blocks of d_k dealt to the warps of the cluster
-  const int kg = warp / S::kSplit, rt0 = (warp % S::kSplit) * kRtw;
   float acc[MT][kRtw][4];
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt)
@@ -327,36 +383,29 @@ adapter_kernel(const AdapterArgs<bf16> p) {
     for (int rt = 0; rt < kRtw; ++rt)
 #pragma unroll
       for (int i = 0; i < 4; ++i) acc[mt][rt][i] = 0.0f;
-  const bf16* w1 = p.w1 + (size_t)a * p.r * p.d_k;
+  uint32_t x[MT][2][8];
 #pragma unroll 1
   for (int kb = (int)rank * kGroups + kg; kb * 64 < p.d_k; kb += (int)ctas * kGroups) {
     const int k = kb * 64 + 16 * q;
-    const bool in0 = k < p.d_k, in1 = k + 8 < p.d_k;
-    uint32_t x[MT][2][8], w[kRtw][8];
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-      for (int h = 0; h < 2; ++h) ld32<S::kSplit == 1>(p.x + (size_t)row_of[mt][h] * p.ldx + k, p.wide_x, in0, in1, x[mt][h]);
+      for (int h = 0; h < 2; ++h) ld32<S::kSplit == 1>(row_at(p.x, row_of[mt][h], x_pitch), k, p.d_k, p.wide_x, x[mt][h]);
+    uint32_t w[kRtw][8];
     if (!TRANS) {
 #pragma unroll
-      for (int rt = 0; rt < kRtw; ++rt) {
-        const int n = (rt0 + rt) * 8 + g;
-        ld32<false>(w1 + (size_t)n * p.d_k + k, p.wide_x, in0 && n < p.r, in1 && n < p.r, w[rt]);
-      }
+      for (int rt = 0; rt < kRtw; ++rt)
+        ld32<false>(w1 + (size_t)min((rt0 + rt) * 8 + g, p.r - 1) * p.d_k, k, p.d_k, p.wide_x, w[rt]);
     } else {
       // rows of [d_k][r]: matrix i holds k = 16 (g / 2) + 2 i + g % 2, so that transposed it holds a lane's k = 16 q + 2 i, + 1
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const int kk = kb * 64 + 16 * (g >> 1) + 2 * i + (g & 1);
-        const bf16* wr = w1 + (size_t)kk * p.r;
-        if (RT == 1) {
-          w[0][i] = kk < p.d_k ? ld4(wr + 2 * q) : 0u;
-        } else if (RT == 2) {
-          const uint2 v = kk < p.d_k ? ld8(wr + 4 * q) : make_uint2(0u, 0u);
-          w[0][i] = v.x; w[kRtw - 1][i] = v.y;
+        const bf16* wr = w1 + (size_t)min(kb * 64 + 16 * (g >> 1) + 2 * i + (g & 1), p.d_k - 1) * p.r;
+        if (kRtw == 1) {
+          w[0][i] = ld4(wr + 2 * q);
         } else {
-          const uint4 v = kk < p.d_k && rt0 * 8 + 8 * q < p.r ? ld_dep16(wr + rt0 * 8 + 8 * q) : make_uint4(0u, 0u, 0u, 0u);
-          w[0][i] = v.x; w[1 % kRtw][i] = v.y; w[2 % kRtw][i] = v.z; w[3 % kRtw][i] = v.w;
+          const uint2 v = ld8(wr + min(rt0 * 8 + 4 * q, p.r - 4));
+          w[0][i] = v.x; w[kRtw - 1][i] = v.y;
         }
       }
 #pragma unroll
@@ -364,62 +413,72 @@ adapter_kernel(const AdapterArgs<bf16> p) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) w[rt][i] = transpose8(w[rt][i]);
     }
+    if (kb * 64 + 64 > p.d_k)
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) clear_tail(x[mt][h], k, p.d_k);
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
       if (DROP && !TRANS)
 #pragma unroll
         for (int h = 0; h < 2; ++h) drop16(x[mt][h], p.drop, row_of[mt][h], k >> 3);
 #pragma unroll
-      for (int rt = 0; rt < kRtw; ++rt)
+      for (int s = 0; s < 4; ++s)
 #pragma unroll
-        for (int s = 0; s < 4; ++s)
+        for (int rt = 0; rt < kRtw; ++rt)
           mma_bf16_16816(acc[mt][rt], x[mt][0][2 * s], x[mt][1][2 * s], x[mt][0][2 * s + 1], x[mt][1][2 * s + 1], w[rt][2 * s], w[rt][2 * s + 1]);
     }
   }
 
   // ---- second product's operands, 64 columns a warp at a time
-  const bf16* w2 = p.w2 + (size_t)a * p.r * p.d_n;
-  const int nb0 = (int)rank * kAdWarps + warp, n_cols = p.out ? p.d_n : 0;
-  uint32_t base[MT][2][8], w[4][RT];
+  constexpr bool kEarly = MT == 1;                       // few rows: both halves' weights at once, the first block's before the sums
+  uint32_t base[MT][2][8], wh[kEarly ? 2 : 1][4][RT];
   auto load_base = [&](int nb) {
     const int c = nb * 64 + 16 * q;
-    const bool in0 = p.base && c < p.d_n, in1 = p.base && c + 8 < p.d_n;
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-      for (int h = 0; h < 2; ++h) ld32<true>(p.base + (size_t)row_of[mt][h] * p.ld_base + c, p.wide_n, in0, in1, base[mt][h]);
+      for (int h = 0; h < 2; ++h) {
+        if (p.base) {
+          ld32<true>(row_at(p.base, row_of[mt][h], base_pitch), c, p.d_n, p.wide_n, base[mt][h]);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) base[mt][h][i] = 0u;
+        }
+      }
   };
   // half 0: the lanes' columns 16 q .. 16 q + 7 (tiles 0 .. 3), half 1: the other eight (4 .. 7)
-  auto load_w = [&](int nb, int half) {
+  auto load_w = [&](int nb, int half, uint32_t (&w)[4][RT]) {
     if (!TRANS) {
       // tile j's column g stands for column 16 (g / 2) + 2 j + g % 2, so that a lane's results are neighbours
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const int c = nb * 64 + 16 * (g >> 1) + 8 * half + 2 * j + (g & 1);
-        const bf16* wr = w2 + (size_t)c * p.r;
+        const bf16* wr = w2 + (size_t)min(nb * 64 + 16 * (g >> 1) + 8 * half + 2 * j + (g & 1), p.d_n - 1) * p.r;
         if (RT == 1) {
-          w[j][0] = c < p.d_n ? ld4(wr + 2 * q) : 0u;
+          w[j][0] = ld4(wr + 2 * q);
         } else if (RT == 2) {
-          const uint2 v = c < p.d_n ? ld8(wr + 4 * q) : make_uint2(0u, 0u);
+          const uint2 v = ld8(wr + 4 * q);
           w[j][0] = v.x; w[j][RT - 1] = v.y;
         } else {
 #pragma unroll
           for (int h = 0; h < RT / 4; ++h) {
-            const uint4 v = c < p.d_n && 32 * h + 8 * q < p.r ? ld_dep16(wr + 32 * h + 8 * q) : make_uint4(0u, 0u, 0u, 0u);
+            const uint4 v = ld_dep16(wr + min(32 * h + 8 * q, p.r - 8));
             w[j][(4 * h) % RT] = v.x; w[j][(4 * h + 1) % RT] = v.y; w[j][(4 * h + 2) % RT] = v.z; w[j][(4 * h + 3) % RT] = v.w;
           }
         }
       }
     } else {
-      const int c = nb * 64 + 16 * q + 8 * half;
+      const int c = min(nb * 64 + 16 * q + 8 * half, p.d_n - 8);
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt) {
-        const uint4 v = rt * 8 + g < p.r && c < p.d_n ? ld_dep16(w2 + (size_t)(rt * 8 + g) * p.d_n + c) : make_uint4(0u, 0u, 0u, 0u);
+        const uint4 v = ld_dep16(w2 + (size_t)min(rt * 8 + g, p.r - 1) * p.d_n + c);
         w[0][rt] = v.x; w[1][rt] = v.y; w[2][rt] = v.z; w[3][rt] = v.w;
       }
     }
   };
-  if (MT == 1 && nb0 * 64 < n_cols) { load_base(nb0); load_w(nb0, 0); }        // few rows: in flight while the sums meet
+  auto load_early = [&](int nb) { load_base(nb); load_w(nb, 0, wh[0]); load_w(nb, 1, wh[kEarly ? 1 : 0]); };
+  if (kEarly && nb0 * 64 < n_cols) load_early(nb0);
 
   // ---- the sums of the block's warps, then of the cluster's blocks, each in a fixed order
   auto quad = [&](int mt, int rt) { return (mt * RT + rt0 + rt) * 32 + lane; };
@@ -440,6 +499,7 @@ adapter_kernel(const AdapterArgs<bf16> p) {
       }
   __syncthreads();
   rc_cluster_wait();                                                           // every peer has started
+#pragma unroll 1
   for (int i = threadIdx.x; i < kQuads; i += kAdThreads) {
     float4 s = part[i];
 #pragma unroll
@@ -447,22 +507,24 @@ adapter_kernel(const AdapterArgs<bf16> p) {
       const float4 v = part[w * kQuads + i];
       s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
     }
+#pragma unroll 1
     for (uint32_t c = 0; c < ctas; ++c) push4(rc_peer(recv + rank * kQuads + i, c), s);
   }
   rc_cluster_arrive();
   rc_cluster_wait();
   const float scale = p.scale ? __ldcg(p.scale + a) : 1.0f;
   const float drop_inv = DROP ? p.drop.inv : 1.0f;
+#pragma unroll 1
   for (int i = threadIdx.x; i < kQuads; i += kAdThreads) {
     float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 1
     for (uint32_t c = 0; c < ctas; ++c) {
       const float4 v = recv[c * kQuads + i];
       s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
     }
     const int l = i & 31, rt = (i >> 5) % RT, mt = (i >> 5) / RT, lg = l >> 2, lq = l & 3;
-    int n0 = rt * 8 + 2 * lq;                                                  // rank of the lane's first column
-    if (TRANS && RT == 2) n0 = 4 * lq + 2 * rt;
-    if (TRANS && RT >= 4) n0 = (rt >> 2) * 32 + 8 * lq + 2 * (rt & 3);
+    // rank of the lane's first column
+    const int n0 = TRANS && RT >= 2 ? (rt & ~1) * 8 + 4 * lq + 2 * (rt & 1) : rt * 8 + 2 * lq;
     const float v[2][2] = {{s.x * drop_inv, s.y * drop_inv}, {s.z * drop_inv, s.w * drop_inv}};
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -482,6 +544,7 @@ adapter_kernel(const AdapterArgs<bf16> p) {
   if (TRANS && p.u_e) {
     uint4* ue = reinterpret_cast<uint4*>(p.u_e) + (size_t)tile * kQuads;
     uint4* uz = reinterpret_cast<uint4*>(p.u_z) + (size_t)tile * kQuads;
+#pragma unroll 1
     for (int i = threadIdx.x; i < kQuads; i += kAdThreads) {
       if ((uint32_t)(i >> 5) % ctas != rank) continue;
       const int l = i & 31, rt = (i >> 5) % RT, mt = (i >> 5) / RT, nn = rt * 8 + (l >> 2), t0 = mt * 16 + 2 * (l & 3);
@@ -498,14 +561,16 @@ adapter_kernel(const AdapterArgs<bf16> p) {
     }
   }
 
-  // ---- second product: [M, r] x [r, d_n], added to base
+  // ---- second product: [M, r] x [r, d_n] on top of base
 #pragma unroll 1
   for (int nb = nb0; nb * 64 < n_cols; nb += (int)ctas * kAdWarps) {
-    if (MT > 1 || nb != nb0) load_base(nb);
     const int c = nb * 64 + 16 * q;
+    if (!kEarly) load_base(nb);
+    else if (nb != nb0) load_early(nb);
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
-      if (MT > 1 || nb != nb0 || half == 1) load_w(nb, half);
+      uint32_t (&w)[4][RT] = wh[kEarly ? half : 0];
+      if (!kEarly) load_w(nb, half, w);
       if (TRANS) {
 #pragma unroll
         for (int j = 0; j < 4; ++j)
@@ -518,7 +583,11 @@ adapter_kernel(const AdapterArgs<bf16> p) {
 #pragma unroll
         for (int j = 0; j < 4; ++j)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) o[j][i] = 0.0f;
+          for (int h = 0; h < 2; ++h) {
+            const uint32_t b = base[mt][h][4 * half + j];
+            o[j][2 * h] = DROP && TRANS ? 0.0f : __uint_as_float(b << 16);
+            o[j][2 * h + 1] = DROP && TRANS ? 0.0f : __uint_as_float(b & 0xffff0000u);
+          }
         const uint16_t* m0 = mid + (mt * 16 + g) * kStride;
         const uint16_t* m1 = m0 + 8 * kStride;
         if (RT == 1) {                               // one MMA: k 0 .. 7 the high part, 8 .. 15 the low part
@@ -551,12 +620,17 @@ adapter_kernel(const AdapterArgs<bf16> p) {
           float v[8];
 #pragma unroll
           for (int j = 0; j < 4; ++j) { v[2 * j] = o[j][2 * h]; v[2 * j + 1] = o[j][2 * h + 1]; }
-          if (DROP && TRANS) drop8(v, drop_draws(p.drop, row_of[mt][h], (c >> 3) + half), p.drop.thr16);
+          if (DROP && TRANS) {
+            drop8(v, drop_draws(p.drop, row_of[mt][h], (c >> 3) + half), p.drop.thr16);
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            uint32_t& b = base[mt][h][4 * half + j];
-            b = pack_bf16x2(v[2 * j] + __uint_as_float(b << 16), v[2 * j + 1] + __uint_as_float(b & 0xffff0000u));
+            for (int j = 0; j < 4; ++j) {
+              const uint32_t b = base[mt][h][4 * half + j];
+              v[2 * j] += __uint_as_float(b << 16);
+              v[2 * j + 1] += __uint_as_float(b & 0xffff0000u);
+            }
           }
+#pragma unroll
+          for (int j = 0; j < 4; ++j) base[mt][h][4 * half + j] = pack_bf16x2(v[2 * j], v[2 * j + 1]);
         }
       }
     }
@@ -564,10 +638,9 @@ adapter_kernel(const AdapterArgs<bf16> p) {
     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const int row = rows[mt * 16 + 8 * h + g];
         const uint32_t (&b)[8] = base[mt][h];
-        bf16* o = p.out + (size_t)row * p.ld_out + c;
-        if (row < 0 || c >= p.d_n) continue;
+        bf16* o = const_cast<bf16*>(row_at(p.out, row_of[mt][h], out_pitch)) + c;
+        if (rows[mt * 16 + 8 * h + g] < 0 || c >= p.d_n) continue;
         if (p.wide_n) {
           asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(o), "r"(b[0]), "r"(b[1]), "r"(b[2]), "r"(b[3]),
                        "r"(b[4]), "r"(b[5]), "r"(b[6]), "r"(b[7]) : "memory");
@@ -581,10 +654,13 @@ adapter_kernel(const AdapterArgs<bf16> p) {
 
 // ---- the gradients of the weights, bf16 ---------------------------------------------------------------------------------
 // G[c][k] = sum over the adapter's rows t of V[t][c] U[t][k]: V = x under its mask with U = s e / (1 - p) for dA, V = g with
-// U = s z for dB.  A block owns kOutCols columns; its warps split the columns four ways and the rows two ways, the
-// blocks of a cluster split the rows further and add their sums through each other's shared memory, in rank order.
-constexpr int kOutColWarps = 4, kOutCols = 64 * kOutColWarps, kOutRowWarps = kAdWarps / kOutColWarps;
-
+// U = s z for dB.  A block owns 256 columns; four warps take 64 of them each, for the first and the second half of a stage's
+// 64 rows.  Two more warps keep a ring of stages full: a bulk copy a row (rows of one adapter lie anywhere), one a lane, and
+// one for the rows' fragments of U, which the kernel above wrote as the MMA wants them.  The columns become the MMA's rows by
+// transposing reads of shared memory, whose rows are 16 bytes apart modulo 128, so that eight of them meet in no bank.
+// The blocks of a cluster split the rows further and add their sums through each other's shared memory, in rank order.
+// Bound: HBM, and at ranks above 32 the MMAs, twice two for every operand pair since U comes in two parts.  Rows by loads into
+// registers had a third of the bytes in flight: 16384 rows x 4096 + 4096, rank 16, 80 us.
 struct OuterSide {
   const void* v; long long ldv;
   const void* u;
@@ -593,41 +669,92 @@ struct OuterSide {
 };
 struct OuterArgs {
   OuterSide side[2];           // 0: dA [n][r][d], 1: dB [n][d][r]
-  int slices0;                 // column slices of side 0
+  int slices[2];               // column slices of either side
   int n_rows, n, r, m;         // m: rows of a tile
   AdTiles tiles;
   Drop drop;
 };
+// Slices of the two sides take turns (the masks make one side the slower), the longer side's rest follows.
+__device__ __forceinline__ void outer_slice(const OuterArgs& p, int i, int& side, int& slice) {
+  const int both = 2 * min(p.slices[0], p.slices[1]);
+  if (i < both) {
+    side = i & 1;
+    slice = i >> 1;
+  } else {
+    side = p.slices[0] > p.slices[1] ? 0 : 1;
+    slice = i - both / 2;
+  }
+}
 
-template <int RT> constexpr int kOutQuads = kOutColWarps * 4 * RT * 32;
-template <int RT> constexpr int kOutSmem = 2 * kOutQuads<RT> * 16;
+// Code of a wait for a copy that ran out in a kernel of this file, until cmoe_adapter_status takes it.
+static __device__ int32_t g_adapter_error;
+// A row of zeros for the places behind a group's last row.
+static __device__ __align__(128) uint32_t g_adapter_zeros[128];
+
+constexpr int kOutColWarps = 4, kOutRowWarps = 2, kOutWidth = 64 * kOutColWarps, kOutStageRows = 64;
+constexpr int kOutCopyWarps = 2, kOutThreads = 32 * (kOutColWarps * kOutRowWarps + kOutCopyWarps);
+constexpr int kOutPitch = kOutWidth * 2 + 16;
+static_assert(kOutStageRows == 32 * kOutCopyWarps && kOutStageRows == 32 * kOutRowWarps, "a copying lane a row, two steps of 16 a warp");
+
+template <int RT> struct OuterShape {
+  static constexpr int kQuads = kOutColWarps * 4 * RT * 32;
+  static constexpr int kV = kOutStageRows * kOutPitch, kU = kOutStageRows / 16 * RT * 512, kStage = kV + kU;
+  static constexpr int kBlocks = RT <= 2 ? 2 : 1, kDepth = RT <= 2 ? 3 : 4;
+  static constexpr int kSmem = kDepth * kStage;            // afterwards: the second half's sums, and those of the peers
+  static_assert(kSmem >= 2 * kQuads * 16 && kBlocks * (kSmem + 2048) <= 227 * 1024, "shared memory of an SM");
+};
+
+__device__ __forceinline__ void bulk_copy(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void ldsm4_t(uint32_t addr, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ uint4 lds16(uint32_t a) {
+  uint4 r;
+  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "r"(a) : "memory");
+  return r;
+}
+__device__ __forceinline__ void sts16(uint32_t a, uint4 v) {
+  asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(a), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
 
 template <int RT, bool DROP>
-__global__ void __launch_bounds__(kAdThreads, RT <= 2 ? 2 : 1)
+__global__ void __launch_bounds__(kOutThreads, OuterShape<RT>::kBlocks)
 adapter_outer_kernel(const OuterArgs p) {
-  constexpr int kQuads = kOutQuads<RT>;
-  extern __shared__ __align__(16) uint8_t smem[];
-  float4* part = reinterpret_cast<float4*>(smem);          // the second half of the rows
-  float4* recv = part + kQuads;                            // [ctas][kQuads / ctas]
+  using S = OuterShape<RT>;
+  constexpr int kQuads = S::kQuads, kDepth = S::kDepth;
+  extern __shared__ __align__(128) uint8_t smem[];
+  __shared__ __align__(8) uint64_t bars[2 * kDepth];       // full, empty
+  __shared__ int32_t stage_rows[kDepth][kOutStageRows];    // the rows of a stage, for their masks
+  __shared__ int abort_word;
+  volatile int* abort_flag = &abort_word;
   const uint32_t ctas = cluster_ctas(), rank = cluster_rank();
-  rc_cluster_arrive();
+  const int warp = warp_index(), lane = threadIdx.x & 31;
+  const uint32_t full0 = smem_u32(bars), empty0 = full0 + 8 * kDepth;
+  if (threadIdx.x == 0) {
+    abort_word = 0;
+    for (int i = 0; i < kDepth; ++i) { mbar_init(full0 + 8 * i, kOutCopyWarps); mbar_init(empty0 + 8 * i, kOutColWarps * kOutRowWarps); }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
   grid_dep_wait();
   grid_dep_trigger();
-  const int side = (int)blockIdx.x < p.slices0 ? 0 : 1, slice = blockIdx.x - (side ? p.slices0 : 0), a = blockIdx.y;
+  int side, slice;
+  outer_slice(p, blockIdx.x, side, slice);
+  const int a = blockIdx.y;
   const OuterSide sd = p.side[side];
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
-  const int cw = warp % kOutColWarps, rw = warp / kOutColWarps;
-  int t_lo = 0, t_hi = (p.n_rows + 15) / 16;               // 16-row tiles
+  long long lo = 0, hi = p.n_rows;                         // places of the adapter's rows in the order of the tiles
   if (p.tiles.row_adapter) {
-    t_lo = __ldcg(p.tiles.tile_start + a) * (p.m / 16);
-    t_hi = __ldcg(p.tiles.tile_start + a + 1) * (p.m / 16);
+    lo = (long long)__ldcg(p.tiles.tile_start + a) * p.m;
+    hi = (long long)__ldcg(p.tiles.tile_start + a + 1) * p.m;
   } else if (a > 0) {
-    t_hi = 0;
+    hi = 0;
   }
-  const int c0 = slice * kOutCols + cw * 64, c = c0 + 16 * q;
-  const bf16* v = (const bf16*)sd.v + c;
-  const uint4* u = (const uint4*)sd.u + lane;
-  const bool drop = DROP && side == 0, in0 = c < sd.d, in1 = c + 8 < sd.d;
+  const int c_lo = slice * kOutWidth, width = min(kOutWidth, sd.d - c_lo);
+  const int n_stages = hi > lo ? (int)((hi - lo + kOutStageRows - 1) / kOutStageRows) : 0;
+  const int mine = n_stages > (int)rank ? (n_stages - (int)rank + (int)ctas - 1) / (int)ctas : 0;     // stages rank, rank + ctas, ..
+  __syncthreads();
+  const bool drop = DROP && side == 0;
   float acc[4][RT][4];
 #pragma unroll
   for (int i = 0; i < 4; ++i)
@@ -635,59 +762,90 @@ adapter_outer_kernel(const OuterArgs p) {
     for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
       for (int e = 0; e < 4; ++e) acc[i][rt][e] = 0.0f;
-  const int step = (int)ctas * kOutRowWarps;
-  // rows of step t; -1: none (nothing is read, and the fragments of U hold zeros there)
-  auto rows_of = [&](int t, int (&row)[2]) {
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const long long pos = (long long)t * 16 + 8 * h + g;
-      row[h] = t >= t_hi ? -1 : p.tiles.row_adapter ? __ldcg(p.tiles.row_list + pos) : pos < p.n_rows ? (int)pos : -1;
+  const int cw = warp % kOutColWarps, rw = warp / kOutColWarps;
+
+  if (warp >= kOutColWarps * kOutRowWarps) {
+    // ---- copies: one row a lane; the first warp's first lane also copies U
+    const int half = warp - kOutColWarps * kOutRowWarps, at = 32 * half + lane;
+    const uint32_t v_pitch = (uint32_t)sd.ldv * 2;
+    auto row_of = [&](int n) {
+      const long long pos = lo + ((long long)n * ctas + rank) * kOutStageRows + at;
+      return n >= mine || pos >= hi ? -1 : p.tiles.row_adapter ? __ldcg(p.tiles.row_list + pos) : (int)pos;
+    };
+    int row = row_of(0), n = 0;
+    bool ok = true;
+    for (; n < mine; ++n) {
+      const int s = n % kDepth, use = n / kDepth, next = row_of(n + 1);
+      if (use > 0 && !mbar_wait_warp(empty0 + 8 * s, (use - 1) & 1, abort_flag, &g_adapter_error, kErrWaitEmpty)) { ok = false; break; }
+      const uint32_t dst = smem_u32(smem) + s * S::kStage, bar = full0 + 8 * s;
+      // 16-row tiles of the stage that U has: the last stage may end early
+      const long long t0 = (lo + ((long long)n * ctas + rank) * kOutStageRows) / 16;
+      const int u_tiles = min(kOutStageRows / 16, (int)((hi + 15) / 16 - t0));
+      stage_rows[s][at] = row;
+      __syncwarp();
+      if (elect_one()) mbar_expect_tx(bar, 32 * width * 2 + (half == 0 ? u_tiles * RT * 512 : 0));
+      __syncwarp();
+      const void* src = row < 0 ? (const void*)g_adapter_zeros : row_at((const bf16*)sd.v, row, v_pitch) + c_lo;
+      bulk_copy(dst + at * kOutPitch, src, width * 2, bar);
+      if (half == 0 && elect_one()) bulk_copy(dst + S::kV, (const uint4*)sd.u + t0 * RT * 32, u_tiles * RT * 512, bar);
+      row = next;
     }
-  };
-  struct Step { uint32_t x[2][8]; uint4 u[RT]; int row[2]; };
-  auto load = [&](int t, const int (&row)[2], Step& s) {
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      s.row[h] = row[h];
-      ld32<true>(v + (size_t)max(row[h], 0) * sd.ldv, sd.wide, row[h] >= 0 && in0, row[h] >= 0 && in1, s.x[h]);
-    }
-    if (t < t_hi)
-#pragma unroll
-      for (int rt = 0; rt < RT; ++rt) s.u[rt] = ld_dep16(u + ((size_t)t * RT + rt) * 32);
-  };
-  if (c0 < sd.d) {
-    int t = t_lo + (int)rank * kOutRowWarps + rw, ahead[2];
-    Step cur, nxt;
-    rows_of(t, ahead);
-    load(t, ahead, cur);
-    rows_of(t + step, ahead);
+    if (!ok)                                               // a wait ran out: what is on its way lands before the block ends
+      for (int i = max(0, n - kDepth); i < n; ++i) {
+        const long long t = clock64();
+        while (!mbar_try_wait(full0 + 8 * (i % kDepth), (i / kDepth) & 1) && clock64() - t < kUmmaWaitCycles) {}
+      }
+  } else {
+    // ---- products: two steps of 16 rows a stage
+    for (int n = 0; n < mine; ++n) {
+      const int s = n % kDepth, use = n / kDepth;
+      if (!mbar_wait_warp(full0 + 8 * s, use & 1, abort_flag, &g_adapter_error, kErrWaitFull)) break;
+      const uint32_t stage = smem_u32(smem) + s * S::kStage;
+      const long long t0 = (lo + ((long long)n * ctas + rank) * kOutStageRows) / 16;
+      const int u_tiles = min(kOutStageRows / 16, (int)((hi + 15) / 16 - t0));
 #pragma unroll 1
-    for (; t < t_hi; t += step) {
-      load(t + step, ahead, nxt);
-      rows_of(t + 2 * step, ahead);
-      if (drop)
+      for (int k = 0; k < 2; ++k) {
+        const int tile = 2 * rw + k;
+        if (tile >= u_tiles || cw * 64 >= width) break;
+        const uint32_t v = stage + tile * 16 * kOutPitch + cw * 128;
+        if (drop) {                                        // the warp's 16 x 64 elements, 16 bytes a lane at a time
 #pragma unroll
-        for (int h = 0; h < 2; ++h) drop16(cur.x[h], p.drop, cur.row[h], c >> 3);
-      // columns become the MMA's rows: tile i has columns 16 (r / 2) + 4 i + r % 2 in its rows r = 0 .. 7, those + 2 in 8 .. 15
+          for (int i = 0; i < 4; ++i) {
+            const int r = 4 * i + (lane >> 3), at = v + r * kOutPitch + (lane & 7) * 16;
+            sts16(at, drop8(lds16(at), drop_draws(p.drop, stage_rows[s][tile * 16 + r], (c_lo >> 3) + cw * 8 + (lane & 7)), p.drop.thr16));
+          }
+          __syncwarp();
+        }
+        uint4 u[RT];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const uint32_t a0 = transpose8(cur.x[0][2 * i]), a1 = transpose8(cur.x[0][2 * i + 1]);
-        const uint32_t a2 = transpose8(cur.x[1][2 * i]), a3 = transpose8(cur.x[1][2 * i + 1]);
+        for (int rt = 0; rt < RT; ++rt) u[rt] = lds16(stage + S::kV + (tile * RT + rt) * 512 + lane * 16);
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt) {
-          mma_bf16_16816(acc[i][rt], a0, a1, a2, a3, cur.u[rt].z, cur.u[rt].w);
-          mma_bf16_16816(acc[i][rt], a0, a1, a2, a3, cur.u[rt].x, cur.u[rt].y);
+        for (int i = 0; i < 4; ++i) {
+          uint32_t x[4];
+          ldsm4_t(v + ((lane & 7) + 8 * (lane >> 4)) * kOutPitch + (16 * i + 8 * ((lane >> 3) & 1)) * 2, x);
+#pragma unroll
+          for (int rt = 0; rt < RT; ++rt) mma_bf16_16816(acc[i][rt], x[0], x[1], x[2], x[3], u[rt].z, u[rt].w);
+#pragma unroll
+          for (int rt = 0; rt < RT; ++rt) mma_bf16_16816(acc[i][rt], x[0], x[1], x[2], x[3], u[rt].x, u[rt].y);
         }
       }
-      cur = nxt;
+      if (drop) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // the stage was written, and is copied over next
+      __syncwarp();
+      if (elect_one()) mbar_arrive(empty0 + 8 * s);
     }
   }
+
+  // ---- the two halves of the rows, then the blocks of the cluster; the ring's memory is free
+  float4* part = reinterpret_cast<float4*>(smem);
+  float4* recv = part + kQuads;                            // [ctas][kQuads / ctas]
   auto quad = [&](int i, int rt) { return ((cw * 4 + i) * RT + rt) * 32 + lane; };
+  __syncthreads();
   if (rw == 1)
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt) part[quad(i, rt)] = make_float4(acc[i][rt][0], acc[i][rt][1], acc[i][rt][2], acc[i][rt][3]);
+  rc_cluster_arrive();                                     // this block no longer copies into its ring
   __syncthreads();
   rc_cluster_wait();
   const int own = kQuads / (int)ctas;                      // quads that a block finishes
@@ -704,25 +862,25 @@ adapter_outer_kernel(const OuterArgs p) {
   rc_cluster_arrive();
   rc_cluster_wait();
   bf16* out = (bf16*)sd.g + (size_t)a * p.r * sd.d;
-  for (int i = threadIdx.x; i < own; i += kAdThreads) {
+  for (int i = threadIdx.x; i < own; i += kOutThreads) {
     float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    for (uint32_t c = 0; c < ctas; ++c) {
-      const float4 w = recv[c * own + i];
+    for (uint32_t k = 0; k < ctas; ++k) {
+      const float4 w = recv[k * own + i];
       s.x += w.x; s.y += w.y; s.z += w.z; s.w += w.w;
     }
     const int k = (int)rank * own + i, l = k & 31, rt = (k >> 5) % RT, mi = (k >> 5) / RT;   // mi: column warp, tile
-    const int n0 = rt * 8 + 2 * (l & 3), lg = l >> 2;
+    const int n0 = rt * 8 + 2 * (l & 3);
     if (n0 >= p.r) continue;
     const float val[2][2] = {{s.x, s.y}, {s.z, s.w}};
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const int c = slice * kOutCols + (mi >> 2) * 64 + 16 * (lg >> 1) + 2 * (2 * (mi & 3) + h) + (lg & 1);
-      if (c >= sd.d) continue;
+      const int col = c_lo + 16 * mi + 8 * h + (l >> 2);
+      if (col >= sd.d) continue;
       if (side == 0) {
-        out[(size_t)n0 * sd.d + c] = __float2bfloat16_rn(val[h][0]);
-        out[(size_t)(n0 + 1) * sd.d + c] = __float2bfloat16_rn(val[h][1]);
+        out[(size_t)n0 * sd.d + col] = __float2bfloat16_rn(val[h][0]);
+        out[(size_t)(n0 + 1) * sd.d + col] = __float2bfloat16_rn(val[h][1]);
       } else {
-        *reinterpret_cast<uint32_t*>(out + (size_t)c * p.r + n0) = pack_bf16x2(val[h][0], val[h][1]);
+        *reinterpret_cast<uint32_t*>(out + (size_t)col * p.r + n0) = pack_bf16x2(val[h][0], val[h][1]);
       }
     }
   }
@@ -927,7 +1085,8 @@ adapter_outer_simt_kernel(const OuterArgs p) {
   grid_dep_wait();
   grid_dep_trigger();
   const int chunks = (p.r + kSimtRc - 1) / kSimtRc;
-  const int side = (int)blockIdx.x < p.slices0 ? 0 : 1, slice = blockIdx.x - (side ? p.slices0 : 0);
+  int side, slice;
+  outer_slice(p, blockIdx.x, side, slice);
   const int a = blockIdx.y / chunks, rc = (blockIdx.y % chunks) * kSimtRc;
   const OuterSide sd = p.side[side];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -1013,29 +1172,30 @@ adapter_outer_simt_kernel(const OuterArgs p) {
 
 inline int adapter_rank_tiles(int r) { return r <= 8 ? 1 : r <= 16 ? 2 : r <= 32 ? 4 : 8; }
 
-// 16-row MMA tiles of a row tile.  Batches whose clusters find their tiles themselves take 16 rows: most of their
-// adapters have a row or two.
-inline int adapter_mt(int, bool small) { return small ? 1 : 2; }
+// 16-row MMA tiles of a row tile: two read the weights half as often; one where the blocks find their tiles themselves (most
+// adapters of such a batch have a row or two) and where the batch would not fill the SMs with eight blocks a tile otherwise.
+inline int adapter_mt(int n_rows, bool small, int n_sms) { return small || n_rows < 4 * n_sms ? 1 : 2; }
 inline bool adapter_small(const int32_t* row_adapter, int n_rows, bool backward) { return row_adapter && n_rows <= kAdSmallRows && !backward; }
-inline int adapter_tile_rows(bool bf, int r, bool small) { return bf ? 16 * adapter_mt(r, small) : kSimtM; }
+inline int adapter_tile_rows(bool bf, int n_rows, bool small, int n_sms) { return bf ? 16 * adapter_mt(n_rows, small, n_sms) : kSimtM; }
 inline long long adapter_max_tiles(long long n_rows, int n, int m, bool one) {
   return one ? (n_rows + m - 1) / m : n_rows / m + std::min<long long>(n + 1, n_rows);
 }
 
+// The layout serves every tile height, so that its size does not depend on the device.
 struct AdapterScratch { size_t tile_start, tile_adapter, row_list, u_e, u_z, total; };
 inline AdapterScratch adapter_scratch(bool bf, int n_rows, int n, int r, bool backward, bool one) {
   AdapterScratch s{};
-  const int m = adapter_tile_rows(bf, r, false);
-  const size_t tiles = (size_t)adapter_max_tiles(n_rows, n, m, one);
+  const int m_lo = bf ? 16 : kSimtM, m_hi = kSimtM;
+  const size_t tiles = (size_t)adapter_max_tiles(n_rows, n, m_lo, one), places = (size_t)adapter_max_tiles(n_rows, n, m_hi, one) * m_hi;
   size_t at = 0;
   const auto take = [&](size_t bytes) { const size_t p = at; at += (bytes + 255) / 256 * 256; return p; };
   if (!one) {
     s.tile_start = take((size_t)(n + 2) * 4);
     s.tile_adapter = take(tiles * 4);
-    s.row_list = take(tiles * m * 4);
+    s.row_list = take(places * 4);
   }
   if (backward) {
-    const size_t u = tiles * m * (bf ? (size_t)adapter_rank_tiles(r) * 32 : (size_t)r * 4);
+    const size_t u = places * (bf ? (size_t)adapter_rank_tiles(r) * 32 : (size_t)r * 4);
     s.u_e = take(u);
     s.u_z = take(u);
   }
@@ -1046,22 +1206,22 @@ inline AdapterScratch adapter_scratch(bool bf, int n_rows, int n, int r, bool ba
 constexpr int kAdSmemPerSm = 220 * 1024;
 constexpr size_t kAdPlainSmem = 46 * 1024;    // dynamic shared memory that needs no attribute next to the kernels' static variables
 
-// Blocks of a cluster for `tiles` tiles that have rows: enough for three blocks an SM, no more than have a `block` wide piece of
-// either product for each warp, and no more than shared memory for their sums allows.
+// Blocks of a cluster for `tiles` tiles: as many as run at once, two an SM; no more than have a `block` wide piece of either
+// product for each warp, and no more than shared memory for their sums allows.
 inline int adapter_ctas(long long tiles, int n_sms, int widest, int block, int smem_limit_ctas) {
   int c = 1;
-  while (c < 8 && tiles * c < 3 * n_sms && c * 2 * kAdWarps <= std::max(kAdWarps, (widest + block - 1) / block) && c * 2 <= smem_limit_ctas) c *= 2;
+  while (c < 8 && tiles * c <= n_sms && c * 2 * kAdWarps <= std::max(kAdWarps, (widest + block - 1) / block) && c * 2 <= smem_limit_ctas) c *= 2;
   return c;
 }
 
-template <typename... KP, typename... A>
-inline cudaError_t launch_cluster(bool dep, void (*kernel)(KP...), dim3 grid, dim3 cluster, size_t smem, cudaStream_t st, A&&... args) {
+template <typename P>
+inline cudaError_t launch_cluster(bool dep, void (*kernel)(P), dim3 grid, dim3 cluster, size_t smem, cudaStream_t st, const P& args, int threads = kAdThreads) {
   if (smem > kAdPlainSmem) {
     const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
   }
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = grid; cfg.blockDim = dim3(kAdThreads); cfg.dynamicSmemBytes = smem; cfg.stream = st;
+  cfg.gridDim = grid; cfg.blockDim = dim3(threads); cfg.dynamicSmemBytes = smem; cfg.stream = st;
   cudaLaunchAttribute at[2];
   unsigned n = 0;
   at[n].id = cudaLaunchAttributeClusterDimension;
@@ -1072,41 +1232,37 @@ inline cudaError_t launch_cluster(bool dep, void (*kernel)(KP...), dim3 grid, di
     at[n++].val.programmaticStreamSerializationAllowed = 1;
   }
   cfg.attrs = at; cfg.numAttrs = n;
-  return cudaLaunchKernelEx(&cfg, kernel, std::forward<A>(args)...);
+  return cudaLaunchKernelEx(&cfg, kernel, args);
 }
 
 template <int MT, int RT, bool TRANS>
-inline cudaError_t launch_adapter_tile(const AdapterArgs<bf16>& a, long long tiles, long long live, int n_sms, bool dep, cudaStream_t st) {
+inline cudaError_t launch_adapter_tile(const AdapterArgs<bf16>& a, bool small, long long tiles, int n_sms, bool dep, cudaStream_t st) {
   using S = AdapterShape<MT, RT, TRANS>;
   const int room = std::max(1, (kAdSmemPerSm / S::kMinBlocks - S::bytes(0)) / S::kRecv);
-  const int ctas = adapter_ctas(live, n_sms, std::max(a.d_k, a.d_n), 64, room);
+  const int ctas = adapter_ctas(tiles, n_sms, std::max(a.d_k, a.d_n), 64, room);
   const size_t smem = S::bytes(ctas);
   const dim3 grid((unsigned)(tiles * ctas)), cl(ctas);
   return a.drop.thr16 ? launch_cluster(dep, adapter_kernel<MT, RT, TRANS, true>, grid, cl, smem, st, a)
                       : launch_cluster(dep, adapter_kernel<MT, RT, TRANS, false>, grid, cl, smem, st, a);
 }
 
-template <bool TRANS>
-inline cudaError_t launch_adapter(const AdapterArgs<bf16>& a, bool small, long long tiles, long long live, int n_sms, bool dep, cudaStream_t st) {
-  const int rt = adapter_rank_tiles(a.r);
-  if constexpr (!TRANS) {
-    if (small) switch (rt) {
-        case 1: return launch_adapter_tile<1, 1, TRANS>(a, tiles, live, n_sms, dep, st);
-        case 2: return launch_adapter_tile<1, 2, TRANS>(a, tiles, live, n_sms, dep, st);
-        case 4: return launch_adapter_tile<1, 4, TRANS>(a, tiles, live, n_sms, dep, st);
-        default: return launch_adapter_tile<1, 8, TRANS>(a, tiles, live, n_sms, dep, st);
-      }
-  }
-  switch (rt) {
-    case 1: return launch_adapter_tile<2, 1, TRANS>(a, tiles, live, n_sms, dep, st);
-    case 2: return launch_adapter_tile<2, 2, TRANS>(a, tiles, live, n_sms, dep, st);
-    case 4: return launch_adapter_tile<2, 4, TRANS>(a, tiles, live, n_sms, dep, st);
-    default: return launch_adapter_tile<2, 8, TRANS>(a, tiles, live, n_sms, dep, st);
+template <int MT, bool TRANS>
+inline cudaError_t launch_adapter_mt(const AdapterArgs<bf16>& a, bool small, long long tiles, int n_sms, bool dep, cudaStream_t st) {
+  switch (adapter_rank_tiles(a.r)) {
+    case 1: return launch_adapter_tile<MT, 1, TRANS>(a, small, tiles, n_sms, dep, st);
+    case 2: return launch_adapter_tile<MT, 2, TRANS>(a, small, tiles, n_sms, dep, st);
+    case 4: return launch_adapter_tile<MT, 4, TRANS>(a, small, tiles, n_sms, dep, st);
+    default: return launch_adapter_tile<MT, 8, TRANS>(a, small, tiles, n_sms, dep, st);
   }
 }
+// m: rows of a tile
 template <bool TRANS>
-inline cudaError_t launch_adapter(const AdapterArgs<float>& a, bool, long long tiles, long long live, int n_sms, bool dep, cudaStream_t st) {
-  const int ctas = adapter_ctas(live, n_sms, std::max(a.d_k, a.d_n), 32, 8);
+inline cudaError_t launch_adapter(const AdapterArgs<bf16>& a, int m, bool small, long long tiles, int n_sms, bool dep, cudaStream_t st) {
+  return m == 16 ? launch_adapter_mt<1, TRANS>(a, small, tiles, n_sms, dep, st) : launch_adapter_mt<2, TRANS>(a, small, tiles, n_sms, dep, st);
+}
+template <bool TRANS>
+inline cudaError_t launch_adapter(const AdapterArgs<float>& a, int, bool small, long long tiles, int n_sms, bool dep, cudaStream_t st) {
+  const int ctas = adapter_ctas(tiles, n_sms, std::max(a.d_k, a.d_n), 32, 8);
   const size_t smem = AdapterSimtSmem::bytes(ctas);
   const dim3 grid((unsigned)(tiles * ctas)), cl(ctas);
   return a.drop.thr16 ? launch_cluster(dep, adapter_simt_kernel<TRANS, true>, grid, cl, smem, st, a)
@@ -1123,20 +1279,27 @@ inline cudaError_t launch_adapter_plan(const AdapterArgs<T>& a, int m, const AdP
   return launch_kernel(false, adapter_plan_kernel, dim3(1), dim3(1024), smem, st, a.tiles.row_adapter, a.n_rows, a.n, m, o);
 }
 
-// Blocks that share an adapter's rows: enough for two rounds of the SMs, and at least four steps for every warp.
-inline int outer_ctas(long long blocks, int n_sms, long long steps) {
-  int c = 1;
-  while (c < 8 && blocks * c < 2 * n_sms && steps >= 8 * c) c *= 2;
-  return c;
+// Blocks that share an adapter's rows: the split with the least rounds of the SMs times steps a block, where a block's start
+// and the sums between blocks cost about twelve steps (16384 rows of four adapters of rank 64 over 5120 + 5120 columns, by one, two,
+// four, eight blocks: 186, 150, 145, 202 us; 16384 rows of one of rank 16 over 4096 + 4096: 309, 160, 84, 50).
+inline int outer_ctas(long long blocks, long long slots, long long steps) {
+  int best = 1;
+  long long least = 0;
+  for (int c = 1; c <= 8; c *= 2) {
+    const long long cost = (blocks * c + slots - 1) / slots * ((steps + c - 1) / c + 12);
+    if (c == 1 || cost < least) { best = c; least = cost; }
+  }
+  return best;
 }
 
 template <int RT> inline cudaError_t launch_outer_rt(OuterArgs p, int n_sms, bool dep, cudaStream_t st) {
-  p.slices0 = (p.side[0].d + kOutCols - 1) / kOutCols;
-  const int slices = p.slices0 + (p.side[1].d + kOutCols - 1) / kOutCols;
-  const int ctas = outer_ctas((long long)slices * p.n, n_sms, (long long)p.n_rows / p.n / (16 * kOutRowWarps));
+  using S = OuterShape<RT>;
+  for (int i = 0; i < 2; ++i) p.slices[i] = (p.side[i].d + kOutWidth - 1) / kOutWidth;
+  const int slices = p.slices[0] + p.slices[1];
+  const int ctas = outer_ctas((long long)slices * p.n, n_sms * S::kBlocks, (long long)p.n_rows / p.n / kOutStageRows);
   const dim3 grid(slices, p.n, ctas), cl(1, 1, ctas);
-  return p.drop.thr16 ? launch_cluster(dep, adapter_outer_kernel<RT, true>, grid, cl, kOutSmem<RT>, st, p)
-                      : launch_cluster(dep, adapter_outer_kernel<RT, false>, grid, cl, kOutSmem<RT>, st, p);
+  return p.drop.thr16 ? launch_cluster(dep, adapter_outer_kernel<RT, true>, grid, cl, S::kSmem, st, p, kOutThreads)
+                      : launch_cluster(dep, adapter_outer_kernel<RT, false>, grid, cl, S::kSmem, st, p, kOutThreads);
 }
 inline cudaError_t launch_outer(bool bf, const OuterArgs& a, int n_sms, bool dep, cudaStream_t st) {
   if (bf) switch (adapter_rank_tiles(a.r)) {
@@ -1146,10 +1309,9 @@ inline cudaError_t launch_outer(bool bf, const OuterArgs& a, int n_sms, bool dep
       default: return launch_outer_rt<8>(a, n_sms, dep, st);
     }
   OuterArgs p = a;
-  p.slices0 = (p.side[0].d + kSimtOutCols - 1) / kSimtOutCols;
-  const int slices = p.slices0 + (p.side[1].d + kSimtOutCols - 1) / kSimtOutCols;
-  const int chunks = (p.r + kSimtRc - 1) / kSimtRc;
-  const int ctas = outer_ctas((long long)slices * p.n * chunks, n_sms, (long long)p.n_rows / p.n / (4 * kAdWarps));
+  for (int i = 0; i < 2; ++i) p.slices[i] = (p.side[i].d + kSimtOutCols - 1) / kSimtOutCols;
+  const int slices = p.slices[0] + p.slices[1], chunks = (p.r + kSimtRc - 1) / kSimtRc;
+  const int ctas = outer_ctas((long long)slices * p.n * chunks, 2 * n_sms, (long long)p.n_rows / p.n / (4 * kAdWarps));
   const dim3 grid(slices, p.n * chunks, ctas), cl(1, 1, ctas);
   return p.drop.thr16 ? launch_cluster(dep, adapter_outer_simt_kernel<true>, grid, cl, 0, st, p)
                       : launch_cluster(dep, adapter_outer_simt_kernel<false>, grid, cl, 0, st, p);

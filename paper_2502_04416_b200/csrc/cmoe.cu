@@ -1430,8 +1430,8 @@ int check_adapters(const cmoe_adapters* ad) {
 
 int check_rows_mat(const Mat& m, int64_t esz, const char* what) {
   if (!m.p) { snprintf(g_last_error, sizeof(g_last_error), "adapters: null %s", what); return CMOE_ERR_INVALID_ARG; }
-  if (m.ld < m.cols || m.ld > (1LL << 40) || (m.ld * esz) % 16 || ((uintptr_t)m.p & 15)) {
-    snprintf(g_last_error, sizeof(g_last_error), "adapters: %s: the row stride is below the width, or it or the pointer is no multiple of 16 bytes", what);
+  if (m.ld < m.cols || m.ld > (1LL << 28) || (m.ld * esz) % 16 || ((uintptr_t)m.p & 15)) {
+    snprintf(g_last_error, sizeof(g_last_error), "adapters: %s: the row stride is below the width or above 2^28, or it or the pointer is no multiple of 16 bytes", what);
     return CMOE_ERR_INVALID_ARG;
   }
   return CMOE_OK;
@@ -1450,8 +1450,8 @@ template <typename T> struct AdapterPass {
   AdapterArgs<T> a{};
   AdPlanOut plan{};
   bool small = false;
-  int m = 0;
-  long long tiles = 0, live = 0;
+  int m = 0, n_sms = 0;
+  long long tiles = 0;
 };
 
 template <typename T>
@@ -1459,29 +1459,27 @@ int plan_adapter_pass(AdapterPass<T>& p, const cmoe_adapters* ad, const int32_t*
                       void* scratch, int64_t scratch_bytes) {
   constexpr bool bf = sizeof(T) == 2;
   p.small = adapter_small(row_adapter, n_rows, backward);
-  p.m = adapter_tile_rows(bf, ad->rank, p.small && bf);
   const bool planned = row_adapter && !p.small;
   const AdapterScratch lay = adapter_scratch(bf, n_rows, ad->n_adapters, ad->rank, backward, !planned);
   if (lay.total > 0) {
     if (!scratch || ((uintptr_t)scratch & 255)) return arg_fail(CMOE_ERR_INVALID_ARG, "adapters: scratch null or not 256-byte aligned");
     if (scratch_bytes < (int64_t)lay.total) return arg_fail(CMOE_ERR_CAPACITY, "adapters: scratch too small");
   }
+  RC_TRY(device_sms(&p.n_sms));
+  p.m = adapter_tile_rows(bf, n_rows, p.small, p.n_sms);
   char* s = static_cast<char*>(scratch);
   p.a.tiles.row_adapter = row_adapter;
   p.a.n_rows = n_rows; p.a.n = ad->n_adapters; p.a.r = ad->rank; p.a.scale = ad->scale;
-  const int live_adapters = std::min(ad->n_adapters, n_rows);
   if (planned) {
     p.plan = {reinterpret_cast<int32_t*>(s + lay.tile_start), reinterpret_cast<int32_t*>(s + lay.tile_adapter),
               reinterpret_cast<int32_t*>(s + lay.row_list)};
     p.a.tiles.planned = 1;
     p.a.tiles.tile_start = p.plan.tile_start; p.a.tiles.tile_adapter = p.plan.tile_adapter; p.a.tiles.row_list = p.plan.row_list;
     p.tiles = adapter_max_tiles(n_rows, ad->n_adapters, p.m, false);
-    p.live = p.tiles;
   } else if (p.small) {
-    p.tiles = n_rows;                                    // every row may head a tile
-    p.live = std::min<long long>(n_rows, live_adapters + n_rows / p.m);
+    p.tiles = std::min<long long>(n_rows, adapter_max_tiles(n_rows, ad->n_adapters, p.m, false));
   } else {
-    p.tiles = p.live = adapter_max_tiles(n_rows, ad->n_adapters, p.m, true);
+    p.tiles = adapter_max_tiles(n_rows, ad->n_adapters, p.m, true);
   }
   if (backward) { p.a.u_e = s + lay.u_e; p.a.u_z = s + lay.u_z; }
   return CMOE_OK;
@@ -1489,7 +1487,7 @@ int plan_adapter_pass(AdapterPass<T>& p, const cmoe_adapters* ad, const int32_t*
 
 template <typename T>
 int adapter_forward_launch(const cmoe_adapters* ad, AdapterPass<T>& p, const Mat& x, const Mat& base, const Mat& out, float* z,
-                           const Drop& drop, int n_sms, cudaStream_t st) {
+                           const Drop& drop, cudaStream_t st) {
   p.a.x = (const T*)x.p; p.a.ldx = x.ld;
   p.a.w1 = (const T*)ad->a; p.a.w2 = (const T*)ad->b;
   p.a.base = (const T*)base.p; p.a.ld_base = base.ld;
@@ -1498,7 +1496,7 @@ int adapter_forward_launch(const cmoe_adapters* ad, AdapterPass<T>& p, const Mat
   p.a.wide_x = wide_rows(x, ad->d_in) && wide_rows({ad->a, ad->d_in, ad->d_in}, ad->d_in);
   p.a.wide_n = wide_rows(base, ad->d_out) && wide_rows(out, ad->d_out);
   if (p.plan.row_list) CU_TRY(launch_adapter_plan(p.a, p.m, p.plan, st));
-  CU_TRY((launch_adapter<false>(p.a, p.small, p.tiles, p.live, n_sms, p.plan.row_list != nullptr, st)));
+  CU_TRY((launch_adapter<false>(p.a, p.m, p.small, p.tiles, p.n_sms, p.plan.row_list != nullptr, st)));
   return CMOE_OK;
 }
 
@@ -1519,9 +1517,7 @@ int adapter_forward_impl(const cmoe_adapters* ad, const Mat& x, const int32_t* r
                          const Mat& out, float* z, void* scratch, int64_t scratch_bytes, cudaStream_t st) {
   AdapterPass<T> p;
   RC_TRY(plan_adapter_pass(p, ad, row_adapter, n_rows, false, scratch, scratch_bytes));
-  int n_sms = 0;
-  RC_TRY(device_sms(&n_sms));
-  return adapter_forward_launch(ad, p, x, base, out, z, drop, n_sms, st);
+  return adapter_forward_launch(ad, p, x, base, out, z, drop, st);
 }
 
 template <typename T>
@@ -1530,8 +1526,6 @@ int adapter_backward_impl(const cmoe_adapters* ad, const Mat& dy, const Mat& x, 
                           int64_t scratch_bytes, cudaStream_t st) {
   AdapterPass<T> p;
   RC_TRY(plan_adapter_pass(p, ad, row_adapter, n_rows, true, scratch, scratch_bytes));
-  int n_sms = 0;
-  RC_TRY(device_sms(&n_sms));
   p.a.x = (const T*)dy.p; p.a.ldx = dy.ld;
   p.a.w1 = (const T*)ad->b; p.a.w2 = (const T*)ad->a;
   p.a.base = (const T*)dx_base.p; p.a.ld_base = dx_base.ld;
@@ -1541,13 +1535,13 @@ int adapter_backward_impl(const cmoe_adapters* ad, const Mat& dy, const Mat& x, 
   p.a.wide_n = wide_rows(dx_base, ad->d_in) && wide_rows(dx, ad->d_in);
   if (!grad_a) p.a.u_e = p.a.u_z = nullptr;
   if (p.plan.row_list) CU_TRY(launch_adapter_plan(p.a, p.m, p.plan, st));
-  CU_TRY((launch_adapter<true>(p.a, false, p.tiles, p.live, n_sms, p.plan.row_list != nullptr, st)));
+  CU_TRY((launch_adapter<true>(p.a, p.m, false, p.tiles, p.n_sms, p.plan.row_list != nullptr, st)));
   if (!grad_a) return CMOE_OK;
   OuterArgs o{};
   o.side[0] = {x.p, x.ld, p.a.u_e, grad_a, ad->d_in, wide_rows(x, ad->d_in)};
   o.side[1] = {dy.p, dy.ld, p.a.u_z, grad_b, ad->d_out, p.a.wide_x};
   o.n_rows = n_rows; o.n = ad->n_adapters; o.r = ad->rank; o.m = p.m; o.tiles = p.a.tiles; o.drop = drop;
-  CU_TRY(launch_outer(sizeof(T) == 2, o, n_sms, true, st));
+  CU_TRY(launch_outer(sizeof(T) == 2, o, p.n_sms, true, st));
   return CMOE_OK;
 }
 }  // namespace
@@ -1647,6 +1641,18 @@ int cmoe_adapter_backward(const cmoe_adapters* ad, const void* dy, int64_t ld_dy
              : adapter_backward_impl<float>(ad, mdy, mx, z, row_adapter, n_rows, d, mb, mo, grad_a, grad_b, scratch, scratch_bytes, st);
 }
 
+int cmoe_adapter_status(int32_t* device_error_word, void* stream) {
+  int32_t w = 0;
+  const int32_t none = 0;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  CU_TRY(cudaMemcpyFromSymbolAsync(&w, g_adapter_error, sizeof(w), 0, cudaMemcpyDeviceToHost, st));
+  CU_TRY(cudaStreamSynchronize(st));
+  if (w) CU_TRY(cudaMemcpyToSymbolAsync(g_adapter_error, &none, sizeof(none), 0, cudaMemcpyHostToDevice, st));
+  if (w) CU_TRY(cudaStreamSynchronize(st));
+  if (device_error_word) *device_error_word = w;
+  return w ? arg_fail(CMOE_ERR_DEVICE_TIMEOUT, "a bounded device-side wait of an adapter kernel ran out") : CMOE_OK;
+}
+
 int cmoe_ffn_forward_adapted(cmoe_layer* L, const void* x, int32_t T, const cmoe_adapters* ad, const int32_t* row_adapter,
                              void* out, void* scratch, int64_t scratch_bytes, void* stream) {
   if (!L) return arg_fail(CMOE_ERR_INVALID_ARG, "null layer");
@@ -1657,13 +1663,11 @@ int cmoe_ffn_forward_adapted(cmoe_layer* L, const void* x, int32_t T, const cmoe
   if (T <= 0) return cmoe_ffn_forward(L, x, T, out, stream);
   const Mat mx{x, d, d}, mo{out, d, d};
   RC_TRY(check_adapter_forward(ad, mx, T, mo, mo, nullptr));
-  int n_sms = 0;
-  RC_TRY(device_sms(&n_sms));
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const auto go = [&](auto pass) -> int {
     RC_TRY(plan_adapter_pass(pass, ad, row_adapter, T, false, scratch, scratch_bytes));
     RC_TRY(cmoe_ffn_forward(L, x, T, out, stream));
-    RC_TRY(adapter_forward_launch(ad, pass, mx, mo, mo, nullptr, Drop{}, n_sms, st));
+    RC_TRY(adapter_forward_launch(ad, pass, mx, mo, mo, nullptr, Drop{}, st));
     L->launches += pass.plan.row_list ? 2 : 1;
     return CMOE_OK;
   };
