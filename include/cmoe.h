@@ -455,9 +455,9 @@ int cmoe_adapter_backward(const cmoe_adapters* ad, const void* dy, int64_t ld_dy
                           int64_t ld_dx_base, void* dx, int64_t ld_dx, void* grad_a, void* grad_b, void* scratch,
                           int64_t scratch_bytes, void* stream);
 
-/* Device-side error word of this device's cmoe_adapter_backward calls: 0, or a code written by a kernel whose bounded wait for
- * a copy ran out (the gradients of that call are undefined).  Synchronises `stream`.  Returns CMOE_ERR_DEVICE_TIMEOUT when the
- * word is non-zero; it is reported once and cleared.  device_error_word may be NULL.  Errors: CUDA. */
+/* Device-side error word of this device's adapter calls (all that are declared above and below): 0, or a code written by a kernel
+ * whose bounded wait inside its block or cluster ran out (the outputs of that call are undefined).  Synchronises `stream`.
+ * Returns CMOE_ERR_DEVICE_TIMEOUT when the word is non-zero; it is reported once and cleared.  device_error_word may be NULL.  Errors: CUDA. */
 int cmoe_adapter_status(int32_t* device_error_word, void* stream);
 
 /* out_t = F_MoE(x_t) + s_a B_a A_a x_t: cmoe_ffn_forward with an adapter per request beside the layer, which all of them share.

@@ -630,7 +630,7 @@ def adapter_backward(dy, x, z, a, b, row_adapter=None, scale=None, dx_base=None,
 
 
 def adapter_status(stream=None) -> int:
-    """cmoe_adapter_status: the current device's error word of the adapters' backward calls (0: none), reported once."""
+    """cmoe_adapter_status: the current device's error word of the adapters' calls (0: none), reported once."""
     w = C.c_int32()
     st = load().cmoe_adapter_status(C.byref(w), _stream_ptr(stream))
     if st not in (0, -6):

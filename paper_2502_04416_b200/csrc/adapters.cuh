@@ -42,26 +42,55 @@ struct AdTiles {
 
 struct AdPlanOut { int32_t *tile_start, *tile_adapter, *row_list; };
 
-// The tiles of a batch, by one block: a stable counting sort of the rows by adapter (so sums over an adapter's rows have
-// a fixed order).  A warp owns a run of rows; lanes with the same adapter find each other by match, so no atomics.
+__device__ __forceinline__ uint32_t cluster_ctas() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+
+// The tiles of a batch, by one cluster of up to eight blocks: a stable counting sort of the rows by adapter (so sums over an
+// adapter's rows have a fixed order).  A warp owns a run of rows; lanes with the same adapter find each other by ballots, so no
+// atomics; blocks exchange their counts.  One block is bound by its instructions and by its stores to many lines (16384 rows of
+// 16 adapters in random order: 20.6 us).
 __global__ void __launch_bounds__(1024)
 adapter_plan_kernel(const int32_t* row_adapter, int n_rows, int n, int m, const AdPlanOut o) {
+  const uint32_t ctas = cluster_ctas(), rank = cluster_rank();
+  rc_cluster_arrive();                       // this block has started
   grid_dep_wait();
   grid_dep_trigger();
   extern __shared__ int32_t sm[];
   const int groups = n + 1;
   int32_t* hist = sm;                        // [32][groups]
-  int32_t* count = hist + 32 * groups;       // [groups]
-  int32_t* tiles = count + groups;           // [groups]
+  int32_t* totals = hist + 32 * groups;      // [8][groups] rows of every block
+  int32_t* count = totals + 8 * groups;      // [groups]
+  int32_t* first = count + groups;           // [groups] place of this block's first row
+  int32_t* tiles = first + groups;           // [groups]
   int32_t* start = tiles + groups;           // [groups + 1]
   int32_t* sums = start + groups + 1;        // [32]
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const unsigned lt = (1u << lane) - 1u;
-  const long long per = (((long long)n_rows + 31) / 32 + 31) / 32 * 32;
-  const long long lo = warp * per, hi = min(lo + per, (long long)n_rows);
+  const long long warps = 32LL * ctas, per = ((n_rows + warps - 1) / warps + 31) / 32 * 32;
+  const long long lo = (long long)(rank * 32 + warp) * per, hi = min(lo + per, (long long)n_rows);
   for (int i = threadIdx.x; i < 32 * groups; i += blockDim.x) hist[i] = 0;
   __syncthreads();
   int32_t* mine = hist + warp * groups;
+  // lanes with the same group: a ballot a bit of its number (match.any takes a turn for every distinct one: 16384 rows of 16
+  // adapters in random order, 22.8 us)
+  const int bits = 32 - __clz(n);
+  const auto same_group = [&](int g) {
+    unsigned same = __ballot_sync(0xffffffffu, g >= 0);
+    if (g < 0) same = ~same;
+    for (int b = 0; b < bits; ++b) {
+      const unsigned set = __ballot_sync(0xffffffffu, g >> b & 1);
+      same &= g >> b & 1 ? set : ~set;
+    }
+    return same;
+  };
   // the groups of 32 kBatch rows from r0 on, their loads in flight at once (-1 behind the warp's last row)
   constexpr int kBatch = 16;
   int v[kBatch];
@@ -78,7 +107,7 @@ adapter_plan_kernel(const int32_t* row_adapter, int n_rows, int n, int m, const 
 #pragma unroll
     for (int i = 0; i < kBatch; ++i) {
       if (r0 + 32 * i >= hi) break;
-      const unsigned same = __match_any_sync(0xffffffffu, v[i]);
+      const unsigned same = same_group(v[i]);
       if (v[i] >= 0 && (same & lt) == 0) mine[v[i]] += __popc(same);
       __syncwarp();
     }
@@ -89,29 +118,42 @@ adapter_plan_kernel(const int32_t* row_adapter, int n_rows, int n, int m, const 
 #pragma unroll 8
     for (int w = 0; w < 32; ++w) { const int c = hist[w * groups + g]; hist[w * groups + g] = run; run += c; }
     count[g] = run;
-    tiles[g] = (run + m - 1) / m;
+  }
+  __syncthreads();
+  rc_cluster_wait();                         // every peer has started
+  for (int g = threadIdx.x; g < groups; g += blockDim.x)
+    for (uint32_t c = 0; c < ctas; ++c) rc_push(rc_peer(totals + rank * groups + g, c), count[g]);
+  rc_cluster_arrive();
+  rc_cluster_wait();
+  for (int g = threadIdx.x; g < groups; g += blockDim.x) {
+    int all = 0, before = 0;
+    for (uint32_t c = 0; c < ctas; ++c) { if (c == rank) before = all; all += totals[c * groups + g]; }
+    count[g] = all;
+    first[g] = before;
+    tiles[g] = (all + m - 1) / m;
   }
   __syncthreads();
   block_scan_groups(tiles, start, groups, sums);
-  for (int g = threadIdx.x; g <= groups; g += blockDim.x) o.tile_start[g] = start[g];
+  if (rank == 0)
+    for (int g = threadIdx.x; g <= groups; g += blockDim.x) o.tile_start[g] = start[g];
   for (long long r0 = lo; r0 < hi; r0 += 32 * kBatch) {
     if (hi - lo > 32 * kBatch) groups_of(r0);            // a warp's only batch is still there
 #pragma unroll
     for (int i = 0; i < kBatch; ++i) {
       if (r0 + 32 * i >= hi) break;
       const int g = v[i];
-      const unsigned same = __match_any_sync(0xffffffffu, g);
+      const unsigned same = same_group(g);
       const int before = g >= 0 ? mine[g] : 0;
       __syncwarp();
       if (g >= 0) {
-        o.row_list[(size_t)start[g] * m + before + __popc(same & lt)] = (int32_t)(r0 + 32 * i + lane);
+        o.row_list[(size_t)start[g] * m + first[g] + before + __popc(same & lt)] = (int32_t)(r0 + 32 * i + lane);
         if ((same & lt) == 0) mine[g] = before + __popc(same);
       }
       __syncwarp();
     }
   }
   const int n_tiles = start[groups];
-  for (int t = threadIdx.x; t < n_tiles; t += blockDim.x) {
+  for (int t = rank * blockDim.x + threadIdx.x; t < n_tiles; t += ctas * blockDim.x) {
     int a = 0, b = groups;                               // start[a] <= t < start[b]
     while (b - a > 1) {
       const int c = (a + b) >> 1;
@@ -121,7 +163,7 @@ adapter_plan_kernel(const int32_t* row_adapter, int n_rows, int n, int m, const 
     for (int i = max(0, count[a] - (t - start[a]) * m); i < m; ++i) o.row_list[(size_t)t * m + i] = -1;
   }
 }
-inline size_t adapter_plan_smem(int n) { return (size_t)(35 * (n + 1) + 1 + 32) * sizeof(int32_t); }
+inline size_t adapter_plan_smem(int n) { return (size_t)(44 * (n + 1) + 1 + 32) * sizeof(int32_t); }
 
 // Rows of tile `tile` into rows[M] (-1: none); returns its adapter, n where its rows have none, or -1: nothing to do.
 // Every thread of the block calls it, and every block of a cluster gets the same answer.
@@ -216,16 +258,6 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t v) {
 __device__ __forceinline__ void push4(uint32_t addr, float4 v) {
   asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
 }
-__device__ __forceinline__ uint32_t cluster_ctas() {
-  uint32_t r;
-  asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
-  return r;
-}
-__device__ __forceinline__ uint32_t cluster_rank() {
-  uint32_t r;
-  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-  return r;
-}
 __device__ __forceinline__ uint32_t ld4(const void* p) {
   uint32_t r;
   asm volatile("ld.global.b32 %0, [%1];" : "=r"(r) : "l"(p));
@@ -238,20 +270,28 @@ __device__ __forceinline__ uint2 ld8(const void* p) {
 }
 
 // Rows without an adapter: base goes to out, z is zero.  The blocks of a cluster share the columns.
-template <typename T>
+template <int THREADS, typename T>
 __device__ __forceinline__ void adapter_none(const AdapterArgs<T>& p, const int32_t* rows, int m, uint32_t rank, uint32_t ctas) {
-  const int vecs = p.d_n / 8;
   const bool copy = p.out && !(p.base == p.out && p.ld_base == p.ld_out);
-  for (int i = 0; i < m; ++i) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, bytes = p.d_n * (int)sizeof(T), pieces = bytes / 16;
+  constexpr int kUnroll = 8;                             // loads in flight a lane
+  for (int i = warp; i < m; i += THREADS / 32) {
     const int row = rows[i];
     if (row < 0) break;
-    if (copy)
-      for (int c = (int)rank * kAdThreads + threadIdx.x; c < vecs; c += kAdThreads * ctas) {
-        float v[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
-        if (p.base) load8(p.base + (size_t)row * p.ld_base + 8 * c, v);
-        store8(p.out + (size_t)row * p.ld_out + 8 * c, v);
+    if (copy) {
+      const uint4* from = reinterpret_cast<const uint4*>(p.base + (size_t)row * p.ld_base);
+      uint4* to = reinterpret_cast<uint4*>(p.out + (size_t)row * p.ld_out);
+      for (int c = (int)rank * 32 * kUnroll + lane; c < pieces; c += 32 * kUnroll * ctas) {
+        uint4 v[kUnroll];
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) v[u] = p.base && c + 32 * u < pieces ? ld_dep16(from + c + 32 * u) : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u)
+          if (c + 32 * u < pieces) to[c + 32 * u] = v[u];
       }
-    if (p.z_out && rank == 0 && (int)threadIdx.x < p.r) p.z_out[(size_t)row * p.r + threadIdx.x] = 0.0f;
+    }
+    if (p.z_out && rank == 0)
+      for (int k = lane; k < p.r; k += 32) p.z_out[(size_t)row * p.r + k] = 0.0f;
   }
 }
 
@@ -332,7 +372,7 @@ adapter_kernel(const AdapterArgs<bf16> p) {
   const int tile = blockIdx.x / ctas;
   const int a = adapter_tile<M>(p.tiles, p.n_rows, p.n, tile, rows);
   if (a < 0 || a == p.n) {                                                     // the whole cluster leaves
-    if (a == p.n) adapter_none(p, rows, M, rank, ctas);
+    if (a == p.n) adapter_none<kAdThreads>(p, rows, M, rank, ctas);
     rc_cluster_wait();
     return;
   }
@@ -724,7 +764,7 @@ __global__ void __launch_bounds__(kOutThreads, OuterShape<RT>::kBlocks)
 adapter_outer_kernel(const OuterArgs p) {
   using S = OuterShape<RT>;
   constexpr int kQuads = S::kQuads, kDepth = S::kDepth;
-  extern __shared__ __align__(128) uint8_t smem[];
+  extern __shared__ __align__(16) uint8_t smem[];
   __shared__ __align__(8) uint64_t bars[2 * kDepth];       // full, empty
   __shared__ int32_t stage_rows[kDepth][kOutStageRows];    // the rows of a stage, for their masks
   __shared__ int abort_word;
@@ -914,7 +954,7 @@ adapter_simt_kernel(const AdapterArgs<float> p) {
   const int tile = blockIdx.x / ctas;
   const int a = adapter_tile<M>(p.tiles, p.n_rows, p.n, tile, rows);
   if (a < 0 || a == p.n) {
-    if (a == p.n) adapter_none(p, rows, M, rank, ctas);
+    if (a == p.n) adapter_none<kAdThreads>(p, rows, M, rank, ctas);
     rc_cluster_wait();
     return;
   }
@@ -1176,16 +1216,26 @@ inline int adapter_rank_tiles(int r) { return r <= 8 ? 1 : r <= 16 ? 2 : r <= 32
 // adapters of such a batch have a row or two) and where the batch would not fill the SMs with eight blocks a tile otherwise.
 inline int adapter_mt(int n_rows, bool small, int n_sms) { return small || n_rows < 4 * n_sms ? 1 : 2; }
 inline bool adapter_small(const int32_t* row_adapter, int n_rows, bool backward) { return row_adapter && n_rows <= kAdSmallRows && !backward; }
-inline int adapter_tile_rows(bool bf, int n_rows, bool small, int n_sms) { return bf ? 16 * adapter_mt(n_rows, small, n_sms) : kSimtM; }
+// Tiles of 128 rows on tcgen05 (adapters_umma.cuh) where ranks make the weights heavy and tiles are filled.  Both sides, us, all
+// kernels of a call, 4096 + 4096 columns (rows x adapters, rank): forward 1024 x 1, 64: 19 against 23; 512 x 1, 64: 20, 16;
+// 2048 x 64, 64: 53, 67; 8192 x 16, 64: 54, 109; 8192 x 16, 32: 53, 77; 4096 x 64, 32: 52, 66; 2048 x 1, 32: 26, 21; 8192 x 8, 16:
+// 53, 51.  Gradients 8192 x 16, 64: 104, 191; 1024 x 16, 64: 69, 87; 2048 x 1, 64: 53, 52; 8192 x 16, 32: 118, 146; 2048 x 64, 32: 183, 150.
+constexpr int kAdTallRows = 128;
+inline bool adapter_tall(bool bf, int n_rows, int n, int r, bool small) {
+  return bf && !small && (r > 32 ? n_rows >= 1024 && n_rows >= 32 * n : r > 16 && n_rows >= 4096 && n_rows >= 64 * n);
+}
+inline int adapter_tile_rows(bool bf, int n_rows, bool small, bool tall, int n_sms) {
+  return tall ? kAdTallRows : bf ? 16 * adapter_mt(n_rows, small, n_sms) : kSimtM;
+}
 inline long long adapter_max_tiles(long long n_rows, int n, int m, bool one) {
   return one ? (n_rows + m - 1) / m : n_rows / m + std::min<long long>(n + 1, n_rows);
 }
 
-// The layout serves every tile height, so that its size does not depend on the device.
+// The layout serves every tile height of the devices, so that its size does not depend on the one in use.
 struct AdapterScratch { size_t tile_start, tile_adapter, row_list, u_e, u_z, total; };
-inline AdapterScratch adapter_scratch(bool bf, int n_rows, int n, int r, bool backward, bool one) {
+inline AdapterScratch adapter_scratch(bool bf, int n_rows, int n, int r, bool backward, bool one, bool tall) {
   AdapterScratch s{};
-  const int m_lo = bf ? 16 : kSimtM, m_hi = kSimtM;
+  const int m_lo = tall ? kAdTallRows : bf ? 16 : kSimtM, m_hi = tall ? kAdTallRows : kSimtM;
   const size_t tiles = (size_t)adapter_max_tiles(n_rows, n, m_lo, one), places = (size_t)adapter_max_tiles(n_rows, n, m_hi, one) * m_hi;
   size_t at = 0;
   const auto take = [&](size_t bytes) { const size_t p = at; at += (bytes + 255) / 256 * 256; return p; };
@@ -1205,6 +1255,14 @@ inline AdapterScratch adapter_scratch(bool bf, int n_rows, int n, int r, bool ba
 
 constexpr int kAdSmemPerSm = 220 * 1024;
 constexpr size_t kAdPlainSmem = 46 * 1024;    // dynamic shared memory that needs no attribute next to the kernels' static variables
+
+// Clusters of c blocks that run at once with per_sm blocks an SM.  Those of four and eight leave places of the processing
+// clusters over: a B200's 148 SMs hold 148, 74, 33, 15 of 1, 2, 4, 8 blocks at one an SM, 296, 148, 71, 33 at two, as the runtime
+// says; one cluster more is another round.
+inline long long clusters_at_once(int n_sms, int c, int per_sm) {
+  const long long places = (long long)n_sms * per_sm;
+  return std::max<long long>(1, c <= 2 ? places / c : per_sm == 1 ? (c == 4 ? places * 9 / 40 : places * 13 / 128) : (c == 4 ? places * 24 / 100 : places * 9 / 80));
+}
 
 // Blocks of a cluster for `tiles` tiles: as many as run at once, two an SM; no more than have a `block` wide piece of either
 // product for each warp, and no more than shared memory for their sums allows.
@@ -1276,17 +1334,26 @@ inline cudaError_t launch_adapter_plan(const AdapterArgs<T>& a, int m, const AdP
     const cudaError_t e = cudaFuncSetAttribute(adapter_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
   }
-  return launch_kernel(false, adapter_plan_kernel, dim3(1), dim3(1024), smem, st, a.tiles.row_adapter, a.n_rows, a.n, m, o);
+  int blocks = 1;                              // a batch of 32 rows or two for every warp
+  while (blocks < 8 && a.n_rows > blocks * 1024) blocks *= 2;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(blocks); cfg.blockDim = dim3(1024); cfg.dynamicSmemBytes = smem; cfg.stream = st;
+  cudaLaunchAttribute at;
+  at.id = cudaLaunchAttributeClusterDimension;
+  at.val.clusterDim.x = blocks; at.val.clusterDim.y = at.val.clusterDim.z = 1;
+  cfg.attrs = &at; cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, adapter_plan_kernel, a.tiles.row_adapter, a.n_rows, a.n, m, o);
 }
 
 // Blocks that share an adapter's rows: the split with the least rounds of the SMs times steps a block, where a block's start
 // and the sums between blocks cost about twelve steps (16384 rows of four adapters of rank 64 over 5120 + 5120 columns, by one, two,
 // four, eight blocks: 186, 150, 145, 202 us; 16384 rows of one of rank 16 over 4096 + 4096: 309, 160, 84, 50).
-inline int outer_ctas(long long blocks, long long slots, long long steps) {
+inline int outer_ctas(long long blocks, int n_sms, int per_sm, long long steps) {
   int best = 1;
   long long least = 0;
   for (int c = 1; c <= 8; c *= 2) {
-    const long long cost = (blocks * c + slots - 1) / slots * ((steps + c - 1) / c + 12);
+    const long long at_once = clusters_at_once(n_sms, c, per_sm);
+    const long long cost = (blocks + at_once - 1) / at_once * ((steps + c - 1) / c + 12);
     if (c == 1 || cost < least) { best = c; least = cost; }
   }
   return best;
@@ -1296,7 +1363,7 @@ template <int RT> inline cudaError_t launch_outer_rt(OuterArgs p, int n_sms, boo
   using S = OuterShape<RT>;
   for (int i = 0; i < 2; ++i) p.slices[i] = (p.side[i].d + kOutWidth - 1) / kOutWidth;
   const int slices = p.slices[0] + p.slices[1];
-  const int ctas = outer_ctas((long long)slices * p.n, n_sms * S::kBlocks, (long long)p.n_rows / p.n / kOutStageRows);
+  const int ctas = outer_ctas((long long)slices * p.n, n_sms, S::kBlocks, (long long)p.n_rows / p.n / kOutStageRows);
   const dim3 grid(slices, p.n, ctas), cl(1, 1, ctas);
   return p.drop.thr16 ? launch_cluster(dep, adapter_outer_kernel<RT, true>, grid, cl, S::kSmem, st, p, kOutThreads)
                       : launch_cluster(dep, adapter_outer_kernel<RT, false>, grid, cl, S::kSmem, st, p, kOutThreads);
@@ -1311,7 +1378,7 @@ inline cudaError_t launch_outer(bool bf, const OuterArgs& a, int n_sms, bool dep
   OuterArgs p = a;
   for (int i = 0; i < 2; ++i) p.slices[i] = (p.side[i].d + kSimtOutCols - 1) / kSimtOutCols;
   const int slices = p.slices[0] + p.slices[1], chunks = (p.r + kSimtRc - 1) / kSimtRc;
-  const int ctas = outer_ctas((long long)slices * p.n * chunks, 2 * n_sms, (long long)p.n_rows / p.n / (4 * kAdWarps));
+  const int ctas = outer_ctas((long long)slices * p.n * chunks, n_sms, 2, (long long)p.n_rows / p.n / (4 * kAdWarps));
   const dim3 grid(slices, p.n * chunks, ctas), cl(1, 1, ctas);
   return p.drop.thr16 ? launch_cluster(dep, adapter_outer_simt_kernel<true>, grid, cl, 0, st, p)
                       : launch_cluster(dep, adapter_outer_simt_kernel<false>, grid, cl, 0, st, p);

@@ -17,6 +17,7 @@
 #include <vector>
 
 #include "adapters.cuh"
+#include "adapters_umma.cuh"
 #include "balance.cuh"
 #include "cluster.cuh"
 #include "combine.cuh"
@@ -1449,7 +1450,7 @@ bool wide_rows(const Mat& m, int64_t width) { return !m.p || (((uintptr_t)m.p & 
 template <typename T> struct AdapterPass {
   AdapterArgs<T> a{};
   AdPlanOut plan{};
-  bool small = false;
+  bool small = false, tall = false;
   int m = 0, n_sms = 0;
   long long tiles = 0;
 };
@@ -1459,14 +1460,15 @@ int plan_adapter_pass(AdapterPass<T>& p, const cmoe_adapters* ad, const int32_t*
                       void* scratch, int64_t scratch_bytes) {
   constexpr bool bf = sizeof(T) == 2;
   p.small = adapter_small(row_adapter, n_rows, backward);
+  p.tall = adapter_tall(bf, n_rows, ad->n_adapters, ad->rank, p.small);
   const bool planned = row_adapter && !p.small;
-  const AdapterScratch lay = adapter_scratch(bf, n_rows, ad->n_adapters, ad->rank, backward, !planned);
+  const AdapterScratch lay = adapter_scratch(bf, n_rows, ad->n_adapters, ad->rank, backward, !planned, p.tall);
   if (lay.total > 0) {
     if (!scratch || ((uintptr_t)scratch & 255)) return arg_fail(CMOE_ERR_INVALID_ARG, "adapters: scratch null or not 256-byte aligned");
     if (scratch_bytes < (int64_t)lay.total) return arg_fail(CMOE_ERR_CAPACITY, "adapters: scratch too small");
   }
   RC_TRY(device_sms(&p.n_sms));
-  p.m = adapter_tile_rows(bf, n_rows, p.small, p.n_sms);
+  p.m = adapter_tile_rows(bf, n_rows, p.small, p.tall, p.n_sms);
   char* s = static_cast<char*>(scratch);
   p.a.tiles.row_adapter = row_adapter;
   p.a.n_rows = n_rows; p.a.n = ad->n_adapters; p.a.r = ad->rank; p.a.scale = ad->scale;
@@ -1485,6 +1487,14 @@ int plan_adapter_pass(AdapterPass<T>& p, const cmoe_adapters* ad, const int32_t*
   return CMOE_OK;
 }
 
+// Both products, by tiles of the height that plan_adapter_pass chose.
+template <bool TRANS, typename T> cudaError_t launch_adapter_pass(const AdapterPass<T>& p, cudaStream_t st) {
+  const bool dep = p.plan.row_list != nullptr;
+  if constexpr (sizeof(T) == 2)
+    if (p.tall) return launch_adapter_umma<TRANS>(p.a, p.tiles, p.n_sms, dep, st);
+  return launch_adapter<TRANS>(p.a, p.m, p.small, p.tiles, p.n_sms, dep, st);
+}
+
 template <typename T>
 int adapter_forward_launch(const cmoe_adapters* ad, AdapterPass<T>& p, const Mat& x, const Mat& base, const Mat& out, float* z,
                            const Drop& drop, cudaStream_t st) {
@@ -1496,7 +1506,7 @@ int adapter_forward_launch(const cmoe_adapters* ad, AdapterPass<T>& p, const Mat
   p.a.wide_x = wide_rows(x, ad->d_in) && wide_rows({ad->a, ad->d_in, ad->d_in}, ad->d_in);
   p.a.wide_n = wide_rows(base, ad->d_out) && wide_rows(out, ad->d_out);
   if (p.plan.row_list) CU_TRY(launch_adapter_plan(p.a, p.m, p.plan, st));
-  CU_TRY((launch_adapter<false>(p.a, p.m, p.small, p.tiles, p.n_sms, p.plan.row_list != nullptr, st)));
+  CU_TRY(launch_adapter_pass<false>(p, st));
   return CMOE_OK;
 }
 
@@ -1535,13 +1545,13 @@ int adapter_backward_impl(const cmoe_adapters* ad, const Mat& dy, const Mat& x, 
   p.a.wide_n = wide_rows(dx_base, ad->d_in) && wide_rows(dx, ad->d_in);
   if (!grad_a) p.a.u_e = p.a.u_z = nullptr;
   if (p.plan.row_list) CU_TRY(launch_adapter_plan(p.a, p.m, p.plan, st));
-  CU_TRY((launch_adapter<true>(p.a, p.m, false, p.tiles, p.n_sms, p.plan.row_list != nullptr, st)));
+  CU_TRY(launch_adapter_pass<true>(p, st));
   if (!grad_a) return CMOE_OK;
   OuterArgs o{};
   o.side[0] = {x.p, x.ld, p.a.u_e, grad_a, ad->d_in, wide_rows(x, ad->d_in)};
   o.side[1] = {dy.p, dy.ld, p.a.u_z, grad_b, ad->d_out, p.a.wide_x};
   o.n_rows = n_rows; o.n = ad->n_adapters; o.r = ad->rank; o.m = p.m; o.tiles = p.a.tiles; o.drop = drop;
-  CU_TRY(launch_outer(sizeof(T) == 2, o, p.n_sms, true, st));
+  CU_TRY(p.tall && ad->rank > kAgLeastRank ? launch_outer_umma(o, p.n_sms, true, st) : launch_outer(sizeof(T) == 2, o, p.n_sms, true, st));
   return CMOE_OK;
 }
 }  // namespace
@@ -1578,7 +1588,9 @@ int cmoe_dropout(const void* x, int64_t ldx, const void* residual, int64_t ld_re
 int64_t cmoe_adapter_scratch_bytes(const cmoe_adapters* ad, int32_t n_rows, int32_t with_row_adapter, int32_t backward) {
   if (check_adapters(ad) != CMOE_OK || n_rows <= 0 || n_rows > kAdMaxRows) return 0;
   const bool planned = with_row_adapter && (backward || n_rows > kAdSmallRows);
-  return (int64_t)adapter_scratch(ad->dtype == CMOE_BF16, n_rows, ad->n_adapters, ad->rank, backward != 0, !planned).total;
+  const bool bf = ad->dtype == CMOE_BF16;
+  const bool tall = adapter_tall(bf, n_rows, ad->n_adapters, ad->rank, with_row_adapter && !planned);
+  return (int64_t)adapter_scratch(bf, n_rows, ad->n_adapters, ad->rank, backward != 0, !planned, tall).total;
 }
 
 int cmoe_adapter_forward(const cmoe_adapters* ad, const void* x, int64_t ldx, const int32_t* row_adapter, int32_t n_rows,

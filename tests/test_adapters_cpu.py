@@ -207,3 +207,16 @@ def test_column_slices_of_one_matrix_do_not_overlap(lib):
 
 def test_adapted_forward_refusals(lib):
     assert lib.cmoe_ffn_forward_adapted(None, P, 1, C.byref(_ad()), None, 2 * P, None, 0, None) == -1
+
+
+def test_scratch_grows_with_the_batch_and_holds_tall_tiles(lib):
+    """A workspace for the longest batch serves the shorter ones, whatever tiles they take; tiles of 128 rows are counted whole."""
+    for n, r, backward in itertools.product((1, 5, 32, 64), (8, 24, 32, 40, 64), (0, 1)):
+        ad = _ad(n_adapters=n, rank=r)
+        sizes = [lib.cmoe_adapter_scratch_bytes(C.byref(ad), rows, 1, backward) for rows in range(300, 9000, 37)]
+        assert sizes == sorted(sizes)
+        for rows in (1024, 2049, 4096, 8191):
+            if r > 16 and rows >= max(64 * n, 4096 if r <= 32 else 1024):
+                tiles = (rows - min(n + 1, rows) + 1 + 127) // 128 + n           # one large group, the others a row each
+                u = 2 * tiles * 128 * (128 if r <= 32 else 256) if backward else 0
+                assert lib.cmoe_adapter_scratch_bytes(C.byref(ad), rows, 1, backward) >= (n + 2) * 4 + tiles * 4 + tiles * 128 * 4 + u
