@@ -114,6 +114,74 @@ dropout_kernel(const DropoutArgs<T> p) {
   }
 }
 
+// The same for a contiguous matrix whose width is no multiple of eight: its elements as one array in vectors of eight, which start
+// at column s past a block's first in a whole row.  A lane draws for the block that its vector starts in and has the keep bits of
+// the next one from the next lane, which starts there, or in the next row's first block; only where both a row's last, short block
+// and the next row's first lie in one vector does it draw twice.  A warp's last lane draws for its neighbour alone.
+// cols >= 16, so that a vector meets two rows at most.
+__device__ __forceinline__ float raw_element(const uint4 (&r)[1], int j) {
+  const uint32_t w = j < 2 ? r[0].x : j < 4 ? r[0].y : j < 6 ? r[0].z : r[0].w;
+  return __uint_as_float(j & 1 ? w & 0xffff0000u : w << 16);
+}
+__device__ __forceinline__ float raw_element(const uint4 (&r)[2], int j) {
+  const uint4& h = r[j >> 2];
+  return __uint_as_float((j & 3) == 0 ? h.x : (j & 3) == 1 ? h.y : (j & 3) == 2 ? h.z : h.w);
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kDropThreads)
+dropout_flat_kernel(const DropoutArgs<T> p) {
+  constexpr int kRaw = sizeof(T) / 2;                                      // 16-byte pieces of a vector
+  const unsigned lane = threadIdx.x & 31, cols = (unsigned)p.cols;
+  const unsigned long long n = (unsigned long long)p.rows * cols, vecs = n >> 3;
+  if (blockIdx.x == 0 && threadIdx.x < (n & 7)) {                          // what no vector takes, of the last row
+    const unsigned long long e = 8 * vecs + threadIdx.x;
+    const unsigned row = (unsigned)p.rows - 1, col = (unsigned)(e - (unsigned long long)row * cols);
+    const bool keep = keep_bits(drop_draws(p.drop, row, col >> 3), p.drop.thr16) >> (col & 7) & 1u;
+    const float x = keep ? to_float(p.x[e]) : 0.0f;
+    p.out[e] = from_float<T>(p.residual ? fmaf(x, p.drop.inv, to_float(p.residual[e])) : x * p.drop.inv);
+  }
+  const unsigned long long warp = ((unsigned long long)blockIdx.x * kDropThreads + threadIdx.x) >> 5;
+  const unsigned long long stride = (unsigned long long)gridDim.x * (kDropThreads / 32) * 31;
+  unsigned long long v = warp * 31 + lane;
+  const unsigned long long row0 = 8 * v / cols, d_row0 = 8 * stride / cols;
+  unsigned row = (unsigned)row0, col = (unsigned)(8 * v - row0 * cols);
+  const unsigned d_row = (unsigned)d_row0, d_col = (unsigned)(8 * stride - d_row0 * cols);
+  for (; v - lane < vecs; v += stride) {
+    const bool in = lane < 31 && v < vecs;
+    uint4 x[kRaw], r[kRaw];
+#pragma unroll
+    for (int i = 0; i < kRaw; ++i) {
+      x[i] = r[i] = make_uint4(0u, 0u, 0u, 0u);
+      if (in) {
+        x[i] = ld_dep16(reinterpret_cast<const uint4*>(p.x) + v * kRaw + i);
+        if (p.residual) r[i] = ld_dep16(reinterpret_cast<const uint4*>(p.residual) + v * kRaw + i);
+      }
+    }
+    const unsigned b = col >> 3, s = col & 7, left = cols - col;          // left: of the vector's first row
+    const uint32_t mine = keep_bits(drop_draws(p.drop, row, b), p.drop.thr16);
+    const uint32_t next = __shfl_down_sync(0xffffffffu, mine, 1);
+    uint32_t bits = mine >> s;
+    if (left > 8) {                                                        // the next lane goes on in this row
+      bits |= next << (8 - s);
+    } else {
+      if (8 * b + 8 < cols) bits |= keep_bits(drop_draws(p.drop, row, b + 1), p.drop.thr16) << (8 - s);
+      bits = (bits & ((1u << left) - 1u)) | next << left;
+    }
+    if (in) {
+      float o[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float kept = bits >> j & 1u ? raw_element(x, j) : 0.0f;
+        o[j] = p.residual ? fmaf(kept, p.drop.inv, raw_element(r, j)) : kept * p.drop.inv;
+      }
+      store8(p.out + 8 * v, o);
+    }
+    row += d_row; col += d_col;
+    if (col >= cols) { col -= cols; ++row; }
+  }
+}
+
 // The same where rows start anywhere: a warp draws for 32 consecutive blocks and walks their 256 elements 32 at a time,
 // one element a lane, so that accesses stay side by side; the blocks' keep bits and places come by shuffles.
 template <typename T>
@@ -162,6 +230,10 @@ template <typename T> inline cudaError_t launch_dropout(const DropoutArgs<T>& a,
   const auto on16 = [](const void* q, long long ld) { return ((uintptr_t)q & 15) == 0 && (ld * sizeof(T)) % 16 == 0; };
   if (on16(a.x, a.ldx) && on16(a.out, a.ld_out) && (!a.residual || on16(a.residual, a.ld_res)))
     return launch_kernel(false, dropout_kernel<T>, dim3(grid), dim3(kDropThreads), 0, st, a);
+  const auto flat = [&](const void* q, long long ld) { return ((uintptr_t)q & 15) == 0 && (ld == a.cols || a.rows == 1); };
+  // 4099 x 1377, bf16, one matrix in and out: 20.0 us by the kernel below, 10.6 by this one (device time)
+  if (a.cols >= 16 && flat(a.x, a.ldx) && flat(a.out, a.ld_out) && (!a.residual || flat(a.residual, a.ld_res)))
+    return launch_kernel(false, dropout_flat_kernel<T>, dim3(drop_grid((unsigned long long)a.rows * a.cols / 8 * 32 / 31 + 1, n_sms)), dim3(kDropThreads), 0, st, a);
   return launch_kernel(false, dropout_ragged_kernel<T>, dim3(grid), dim3(kDropThreads), 0, st, a);
 }
 

@@ -144,3 +144,23 @@ def test_argument_checks():
         binding.dropout(x, Dropout(1.0))
     assert e.value.status == -1
     assert binding.dropout(x[:0], Dropout(0.1)).shape == (0, 16) and binding.dropout(x[:, :0], Dropout(0.1)).shape == (8, 0)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_contiguous_rows_of_any_width(dtype):
+    """Widths whose rows start inside a vector of the flat array, at every place of it, in batches that end inside one; the same
+    values from a matrix that starts off a 16-byte boundary, and nothing written behind the last element."""
+    import torch
+    for cols in list(range(9, 42)) + [255, 257, 511, 1001]:
+        for rows in (1, 2, 67):
+            x, r = _rand((rows, cols), dtype, cols), _rand((rows, cols), dtype, cols + 1)
+            drop = Dropout(0.3, 2**40 + cols, 2**35, 11)
+            keep = ao.keep_mask(rows, cols, 0.3, drop.seed, drop.offset, 11)
+            room = torch.full((rows * cols + 16,), 7.0, dtype=x.dtype, device="cuda")
+            got = binding.dropout(x, drop, out=room[:rows * cols].view(rows, cols))
+            np.testing.assert_array_equal(_host(got) != 0, keep & (_host(x) != 0))
+            assert (room[rows * cols:] == 7).all()
+            both = binding.dropout(x, drop, residual=r)
+            _check(both, ao.dropout(_host(x), 0.3, drop.seed, drop.offset, 11, _host(r)), np.abs(_host(x)) * 1.43 + np.abs(_host(r)), dtype)
+            off = torch.empty(rows * cols + 1, dtype=x.dtype, device="cuda")[1:].view(rows, cols).copy_(x)
+            assert torch.equal(binding.dropout(off, drop, residual=r), both)
