@@ -92,7 +92,7 @@ adapter_plan_kernel(const int32_t* row_adapter, int n_rows, int n, int m, const 
     return same;
   };
   // the groups of 32 kBatch rows from r0 on, their loads in flight at once (-1 behind the warp's last row)
-  constexpr int kBatch = 16;
+  constexpr int kBatch = 4;
   int v[kBatch];
   auto groups_of = [&](long long r0) {
 #pragma unroll
