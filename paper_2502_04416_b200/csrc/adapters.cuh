@@ -8,10 +8,10 @@
 // of one adapter and never writes the middle to global memory unless it is wanted; a second kernel forms the two
 // gradients of the weights, sums over the rows of an adapter.
 //
-// Bound: HBM (rows read once, outputs written once; 2 r flops an element).  At a rank of 64 that is 64 flops a byte, a
-// quarter of what the tensor cores could do at this bandwidth, so the products are warp-level MMAs on fragments that are
-// loaded straight from global memory, 16 bytes a lane: no staging through shared memory, and a lane's 16 bytes are the
-// eight elements that share one block of the dropout generator, so the mask costs no exchange either.
+// Bound: HBM (rows read once, outputs written once; 2 r flops an element).  The products here are warp-level MMAs on fragments
+// that are loaded straight from global memory, 32 bytes a lane: no staging through shared memory, and a lane's bytes are
+// elements that share blocks of the dropout generator, so the mask costs no exchange either.  Where ranks are high and batches
+// long, weights and MMAs weigh more than the rows, and tiles of 128 rows on tcgen05 take over (adapters_umma.cuh).
 #pragma once
 
 #include "common.cuh"
@@ -705,7 +705,7 @@ struct OuterSide {
   const void* v; long long ldv;
   const void* u;
   void* g;
-  int d, wide;
+  int d;
 };
 struct OuterArgs {
   OuterSide side[2];           // 0: dA [n][r][d], 1: dB [n][d][r]
@@ -1294,7 +1294,7 @@ inline cudaError_t launch_cluster(bool dep, void (*kernel)(P), dim3 grid, dim3 c
 }
 
 template <int MT, int RT, bool TRANS>
-inline cudaError_t launch_adapter_tile(const AdapterArgs<bf16>& a, bool small, long long tiles, int n_sms, bool dep, cudaStream_t st) {
+inline cudaError_t launch_adapter_tile(const AdapterArgs<bf16>& a, long long tiles, int n_sms, bool dep, cudaStream_t st) {
   using S = AdapterShape<MT, RT, TRANS>;
   const int room = std::max(1, (kAdSmemPerSm / S::kMinBlocks - S::bytes(0)) / S::kRecv);
   const int ctas = adapter_ctas(tiles, n_sms, std::max(a.d_k, a.d_n), 64, room);
@@ -1305,21 +1305,21 @@ inline cudaError_t launch_adapter_tile(const AdapterArgs<bf16>& a, bool small, l
 }
 
 template <int MT, bool TRANS>
-inline cudaError_t launch_adapter_mt(const AdapterArgs<bf16>& a, bool small, long long tiles, int n_sms, bool dep, cudaStream_t st) {
+inline cudaError_t launch_adapter_mt(const AdapterArgs<bf16>& a, long long tiles, int n_sms, bool dep, cudaStream_t st) {
   switch (adapter_rank_tiles(a.r)) {
-    case 1: return launch_adapter_tile<MT, 1, TRANS>(a, small, tiles, n_sms, dep, st);
-    case 2: return launch_adapter_tile<MT, 2, TRANS>(a, small, tiles, n_sms, dep, st);
-    case 4: return launch_adapter_tile<MT, 4, TRANS>(a, small, tiles, n_sms, dep, st);
-    default: return launch_adapter_tile<MT, 8, TRANS>(a, small, tiles, n_sms, dep, st);
+    case 1: return launch_adapter_tile<MT, 1, TRANS>(a, tiles, n_sms, dep, st);
+    case 2: return launch_adapter_tile<MT, 2, TRANS>(a, tiles, n_sms, dep, st);
+    case 4: return launch_adapter_tile<MT, 4, TRANS>(a, tiles, n_sms, dep, st);
+    default: return launch_adapter_tile<MT, 8, TRANS>(a, tiles, n_sms, dep, st);
   }
 }
 // m: rows of a tile
 template <bool TRANS>
-inline cudaError_t launch_adapter(const AdapterArgs<bf16>& a, int m, bool small, long long tiles, int n_sms, bool dep, cudaStream_t st) {
-  return m == 16 ? launch_adapter_mt<1, TRANS>(a, small, tiles, n_sms, dep, st) : launch_adapter_mt<2, TRANS>(a, small, tiles, n_sms, dep, st);
+inline cudaError_t launch_adapter(const AdapterArgs<bf16>& a, int m, long long tiles, int n_sms, bool dep, cudaStream_t st) {
+  return m == 16 ? launch_adapter_mt<1, TRANS>(a, tiles, n_sms, dep, st) : launch_adapter_mt<2, TRANS>(a, tiles, n_sms, dep, st);
 }
 template <bool TRANS>
-inline cudaError_t launch_adapter(const AdapterArgs<float>& a, int, bool small, long long tiles, int n_sms, bool dep, cudaStream_t st) {
+inline cudaError_t launch_adapter(const AdapterArgs<float>& a, int, long long tiles, int n_sms, bool dep, cudaStream_t st) {
   const int ctas = adapter_ctas(tiles, n_sms, std::max(a.d_k, a.d_n), 32, 8);
   const size_t smem = AdapterSimtSmem::bytes(ctas);
   const dim3 grid((unsigned)(tiles * ctas)), cl(ctas);
@@ -1347,7 +1347,8 @@ inline cudaError_t launch_adapter_plan(const AdapterArgs<T>& a, int m, const AdP
 
 // Blocks that share an adapter's rows: the split with the least rounds of the SMs times steps a block, where a block's start
 // and the sums between blocks cost about twelve steps (16384 rows of four adapters of rank 64 over 5120 + 5120 columns, by one, two,
-// four, eight blocks: 186, 150, 145, 202 us; 16384 rows of one of rank 16 over 4096 + 4096: 309, 160, 84, 50).
+// four, eight blocks: 179, 140, 161, 209 us; 4096 rows of one of rank 32 over 4096 + 4096: 84, 46, 27, 45; of rank 8 under a
+// mask: 120, 63, 36, 30).
 inline int outer_ctas(long long blocks, int n_sms, int per_sm, long long steps) {
   int best = 1;
   long long least = 0;

@@ -1492,7 +1492,7 @@ template <bool TRANS, typename T> cudaError_t launch_adapter_pass(const AdapterP
   const bool dep = p.plan.row_list != nullptr;
   if constexpr (sizeof(T) == 2)
     if (p.tall) return launch_adapter_umma<TRANS>(p.a, p.tiles, p.n_sms, dep, st);
-  return launch_adapter<TRANS>(p.a, p.m, p.small, p.tiles, p.n_sms, dep, st);
+  return launch_adapter<TRANS>(p.a, p.m, p.tiles, p.n_sms, dep, st);
 }
 
 template <typename T>
@@ -1548,8 +1548,8 @@ int adapter_backward_impl(const cmoe_adapters* ad, const Mat& dy, const Mat& x, 
   CU_TRY(launch_adapter_pass<true>(p, st));
   if (!grad_a) return CMOE_OK;
   OuterArgs o{};
-  o.side[0] = {x.p, x.ld, p.a.u_e, grad_a, ad->d_in, wide_rows(x, ad->d_in)};
-  o.side[1] = {dy.p, dy.ld, p.a.u_z, grad_b, ad->d_out, p.a.wide_x};
+  o.side[0] = {x.p, x.ld, p.a.u_e, grad_a, ad->d_in};
+  o.side[1] = {dy.p, dy.ld, p.a.u_z, grad_b, ad->d_out};
   o.n_rows = n_rows; o.n = ad->n_adapters; o.r = ad->rank; o.m = p.m; o.tiles = p.a.tiles; o.drop = drop;
   CU_TRY(p.tall && ad->rank > kAgLeastRank ? launch_outer_umma(o, p.n_sms, true, st) : launch_outer(sizeof(T) == 2, o, p.n_sms, true, st));
   return CMOE_OK;

@@ -6,8 +6,9 @@ import numpy as np
 import pytest
 
 from oracle import adapters_oracle as ao
-from paper_2502_04416_b200 import binding
+from paper_2502_04416_b200 import binding, workloads as wl
 from paper_2502_04416_b200.binding import Dropout
+from tests import parity
 from tests.test_gpu_adapters import check_backward, check_forward, make
 
 pytestmark = pytest.mark.gpu
@@ -188,3 +189,20 @@ def test_long_batch():
         bound = 2.0**-9 * want.abs() + 1.01 * (((2 * rows / 8 + 64) * 2.0**-23 + 2.0**-15 + 2.0**-21) * mag + (d_out / 8 + 64) * 2.0**-23 * e_mag)
         assert ((ga[i][:, cols].double() - want).abs() <= bound).all()
         del e
+
+
+@pytest.mark.parametrize("mixed", [True, False])
+def test_beside_a_layer(mixed):
+    import torch
+    rows = 1100
+    inp = wl.make_inputs(wl.Workload("adapted", wl.LayerShape(256, 1024, 8, 2, 2, "bf16"), (rows,), seed=3))
+    layer = parity.gpu_layer(inp.layers[0], rows)
+    x = parity.to_device(inp.x, "bf16")
+    s = make("bf16", rows, 5, 40, 256, 256, ids="mixed" if mixed else None, seed=1)
+    plain = layer.forward(x)
+    want = binding.adapter_forward(x, s["a"], s["b"], s["ids"], s["scale"], base=plain)
+    for _ in range(2):
+        assert torch.equal(layer.forward_adapted(x, s["a"], s["b"], s["ids"], s["scale"]), want)
+    s["x"], s["base"] = x, plain
+    check_forward(s, "bf16", want, None)
+    layer.destroy()
