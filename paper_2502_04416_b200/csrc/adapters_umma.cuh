@@ -662,6 +662,10 @@ inline cudaError_t launch_outer_umma(OuterArgs p, int n_sms, bool dep, cudaStrea
   // 4096 + 4096: 173, 93, 54, 40 us; 1024 rows of one over 5120 + 5120: 40, 27, 22, 33 us).
   int ctas = 1;
   while (ctas < 8 && (long long)slices * p.n * ctas * 2 < 3LL * n_sms && p.n_rows / p.n >= 512 * ctas) ctas *= 2;
+  // Rows of several adapters are seldom shared evenly: two adapters that have nearly all of them should fill the SMs as well, where
+  // there are enough of them to pay for more blocks (by 2 and 4 blocks, 16384 rows in random shares of four adapters: 102, 95 us;
+  // by 1 and 2, 8192 rows of eight adapters, 4096 + 4096: random shares 64, 50, even ones 38, 50).
+  while (p.n > 1 && ctas < 8 && 4LL * slices * ctas < 3LL * n_sms && p.n_rows / p.n >= 2048 * ctas) ctas *= 2;
   const dim3 grid(slices, p.n, ctas), cl(1, 1, ctas);
   return p.drop.thr16 ? launch_cluster(dep, adapter_outer_umma_kernel<true>, grid, cl, kAgSmem, st, p, kAuThreads)
                       : launch_cluster(dep, adapter_outer_umma_kernel<false>, grid, cl, kAgSmem, st, p, kAuThreads);
