@@ -929,7 +929,7 @@ adapter_outer_kernel(const OuterArgs p) {
 // ---- fp32 -------------------------------------------------------------------------------------------------------------
 // The same tiles and exchange on the CUDA cores, with fused multiply-adds in full 32 bits.  A lane holds rows g, g + 8, ..
 // of the tile and eight neighbouring k (first product) or columns (second product); ranks go by in chunks of 16.
-constexpr int kSimtM = 32, kSimtRc = 16;
+constexpr int kSimtM = 32, kSimtRc = 16, kSimtBatch = 2;
 struct AdapterSimtSmem {
   static constexpr int kStride = kAdMaxRank + 4;
   static constexpr int bytes(int ctas) {
@@ -983,15 +983,22 @@ adapter_simt_kernel(const AdapterArgs<float> p) {
           if (DROP && !TRANS) drop8(x[m], drop_draws(p.drop, row_of[m], k >> 3), p.drop.thr16);
         }
         if (!TRANS) {
+          // ranks come in eights; a few at a time, so that their loads are in flight together
 #pragma unroll
-          for (int j = 0; j < kSimtRc; ++j)
-            if (rc + j < p.r) {
-              float w[8];
-              load8(w1 + (size_t)(rc + j) * p.d_k + k, w);
+          for (int h = 0; h < kSimtRc / 8; ++h)
+            if (rc + 8 * h < p.r) {
 #pragma unroll
-              for (int m = 0; m < 4; ++m)
+              for (int j0 = 8 * h; j0 < 8 * h + 8; j0 += kSimtBatch) {
+                float w[kSimtBatch][8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) acc[m][j] = fmaf(x[m][i], w[i], acc[m][j]);
+                for (int j = 0; j < kSimtBatch; ++j) load8(w1 + (size_t)(rc + j0 + j) * p.d_k + k, w[j]);
+#pragma unroll
+                for (int j = 0; j < kSimtBatch; ++j)
+#pragma unroll
+                  for (int m = 0; m < 4; ++m)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) acc[m][j0 + j] = fmaf(x[m][i], w[j][i], acc[m][j0 + j]);
+              }
             }
         } else {
 #pragma unroll
