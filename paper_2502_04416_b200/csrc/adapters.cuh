@@ -1118,14 +1118,15 @@ adapter_simt_kernel(const AdapterArgs<float> p) {
   }
 }
 
-// Gradients of the weights in fp32: a block owns 64 columns and 16 ranks (two columns a lane), its warps and the blocks
-// of its cluster split the rows.  The masks of four rows come from one generator block a lane, by shuffles.
-constexpr int kSimtOutCols = 64;
+// Gradients of the weights in fp32: a block owns 128 columns and 16 ranks (four columns a lane: with two, the loads of the narrow
+// operand took as long as the products; 8192 rows x 4096 + 4096, rank 64, 910 us), its warps and the blocks of its cluster split
+// the rows.  The masks of four rows come from two generator blocks a lane, by shuffles.
+constexpr int kSimtOutCols = 128;
 
 template <bool DROP>
 __global__ void __launch_bounds__(kAdThreads, 2)
 adapter_outer_simt_kernel(const OuterArgs p) {
-  __shared__ __align__(16) float part[kAdWarps][kSimtRc][kSimtOutCols];
+  __shared__ __align__(16) float part[kAdWarps / 2][kSimtRc][kSimtOutCols];
   __shared__ __align__(16) float recv[kSimtRc * kSimtOutCols];       // [ctas][kSimtRc * kSimtOutCols / ctas]
   const uint32_t ctas = cluster_ctas(), rank = cluster_rank();
   rc_cluster_arrive();
@@ -1146,51 +1147,62 @@ adapter_outer_simt_kernel(const OuterArgs p) {
   }
   const float* v = (const float*)sd.v;
   const float* u = (const float*)sd.u;
-  const int c = slice * kSimtOutCols + 2 * lane;
+  const int c = slice * kSimtOutCols + 4 * lane;         // widths are multiples of 8: four columns are in or out together
   const bool in = c < sd.d, drop = DROP && side == 0;
-  float acc[2][kSimtRc];
+  float acc[4][kSimtRc];
 #pragma unroll
-  for (int j = 0; j < kSimtRc; ++j) acc[0][j] = acc[1][j] = 0.0f;
+  for (int j = 0; j < kSimtRc; ++j) acc[0][j] = acc[1][j] = acc[2][j] = acc[3][j] = 0.0f;
   const int stride = (int)ctas * kAdWarps * 4;
 #pragma unroll 1
   for (int t = lo + ((int)rank * kAdWarps + warp) * 4; t < hi; t += stride) {
     int row[4];
-    uint2 x[4];
+    uint4 x[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       row[i] = t + i < hi ? (p.tiles.row_adapter ? __ldcg(p.tiles.row_list + t + i) : t + i) : -1;
-      x[i] = row[i] >= 0 && in ? ld8(v + (size_t)row[i] * sd.ldv + c) : make_uint2(0u, 0u);
+      x[i] = row[i] >= 0 && in ? ld_dep16(v + (size_t)row[i] * sd.ldv + c) : make_uint4(0u, 0u, 0u, 0u);
     }
-    uint32_t bits = 0;
-    if (drop) {
-      const int mine = (lane >> 3) == 0 ? row[0] : (lane >> 3) == 1 ? row[1] : (lane >> 3) == 2 ? row[2] : row[3];
-      bits = keep_bits(drop_draws(p.drop, mine, (slice * kSimtOutCols >> 3) + (lane & 7)), p.drop.thr16);
-    }
+    uint32_t bits[2] = {0u, 0u};                                     // of rows lane / 16 and 2 + lane / 16, block lane % 16
+    if (drop)
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        bits[h] = keep_bits(drop_draws(p.drop, lane < 16 ? row[2 * h] : row[2 * h + 1], (slice * kSimtOutCols >> 3) + (lane & 15)), p.drop.thr16);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       if (drop) {
-        const uint32_t b = __shfl_sync(0xffffffffu, bits, 8 * i + (lane >> 2)) >> (2 * (lane & 3));
+        const uint32_t b = __shfl_sync(0xffffffffu, bits[i >> 1], 16 * (i & 1) + (lane >> 1)) >> (4 * (lane & 1));
         if (!(b & 1u)) x[i].x = 0u;
         if (!(b & 2u)) x[i].y = 0u;
+        if (!(b & 4u)) x[i].z = 0u;
+        if (!(b & 8u)) x[i].w = 0u;
       }
       if (row[i] < 0) continue;
-      const float x0 = __uint_as_float(x[i].x), x1 = __uint_as_float(x[i].y);
+      const float xs[4] = {__uint_as_float(x[i].x), __uint_as_float(x[i].y), __uint_as_float(x[i].z), __uint_as_float(x[i].w)};
 #pragma unroll
       for (int h = 0; h < kSimtRc / 8; ++h)
         if (rc + 8 * h < p.r) {
           float w[8];
           load8(u + (size_t)(t + i) * p.r + rc + 8 * h, w);
 #pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            acc[0][8 * h + j] = fmaf(x0, w[j], acc[0][8 * h + j]);
-            acc[1][8 * h + j] = fmaf(x1, w[j], acc[1][8 * h + j]);
-          }
+          for (int j = 0; j < 8; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[e][8 * h + j] = fmaf(xs[e], w[j], acc[e][8 * h + j]);
         }
     }
   }
+  // the second half of the warps, then the first on top
 #pragma unroll
-  for (int j = 0; j < kSimtRc; ++j) *reinterpret_cast<float2*>(&part[warp][j][2 * lane]) = make_float2(acc[0][j], acc[1][j]);
-  __syncthreads();
+  for (int turn = 1; turn >= 0; --turn) {
+    if (warp / (kAdWarps / 2) == turn)
+#pragma unroll
+      for (int j = 0; j < kSimtRc; ++j) {
+        float4& s = *reinterpret_cast<float4*>(&part[warp % (kAdWarps / 2)][j][4 * lane]);
+        float4 f = make_float4(acc[0][j], acc[1][j], acc[2][j], acc[3][j]);
+        if (turn == 0) { f.x += s.x; f.y += s.y; f.z += s.z; f.w += s.w; }
+        s = f;
+      }
+    __syncthreads();
+  }
   rc_cluster_wait();
   constexpr int kAll = kSimtRc * kSimtOutCols;
   const int own = kAll / (int)ctas;
@@ -1198,7 +1210,7 @@ adapter_outer_simt_kernel(const OuterArgs p) {
   for (int i = 4 * threadIdx.x; i < kAll; i += 4 * kAdThreads) {
     float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll
-    for (int w = 0; w < kAdWarps; ++w) {
+    for (int w = 0; w < kAdWarps / 2; ++w) {
       const float4 f = *reinterpret_cast<const float4*>(flat + w * kAll + i);
       s.x += f.x; s.y += f.y; s.z += f.z; s.w += f.w;
     }
