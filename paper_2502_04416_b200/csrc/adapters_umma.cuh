@@ -4,6 +4,8 @@
 // warp-level MMAs of the two-part middle take as long as HBM does.  Here 128 rows share the weights and the tensor cores
 // read everything from shared memory: X [128 x 64] and W1 [64 x r] give the middle in tensor memory, its two bf16 parts go
 // back to shared memory as the A operand, and blocks of 64 output columns meet the rows' base in the epilogue.
+// Bound: HBM latency at the start and the end of a block (9 us with nothing in between), then HBM: 16384 rows of four adapters, rank
+// 64, 5120 + 5120 columns 101 us, 5 TB/s; by tiles of 32 rows 266 us.
 // Blocks of a cluster share the columns of both products and exchange the middle's sums, 1 / ctas of the rows each, in rank order.
 //
 // Every operand comes by 16-byte cp.async into 128-byte rows with the 128-byte swizzle: rows of one adapter lie anywhere, widths
@@ -404,9 +406,11 @@ adapter_umma_kernel(const AdapterArgs<bf16> p) {
 // ---- the gradients of the weights ---------------------------------------------------------------------------------------
 // G[k][c] = sum over the adapter's rows t of U[t][k] V[t][c], as adapter_outer_kernel, for the tiles above: U's rows [32 x 64],
 // high and low parts, are 128 rows of the product, V's [32 x 256] its columns; both as they lie in memory (the sum runs along
-// their rows: operands whose columns are neighbours).  With V as the rows and U as 64 columns an MMA took about 160 cycles and
-// bound the pass.  U was written in the swizzled order and comes by bulk copies.  Two blocks an SM, so that one's start and
-// end are the other's time.  Blocks of a cluster split the rows and add their sums through shared memory, in rank order.
+// their rows: operands whose columns are neighbours).  Two MMAs of 256 columns a step; with V as the rows and U as 64 columns they
+// were eight.  U was written in the swizzled order and comes by bulk copies.  Two blocks an SM, so that one's start and end (13 us
+// with a cluster) are the other's time.  Blocks of a cluster split the rows and add their sums through shared memory, in rank order.
+// Bound: the bytes a block has in flight, 4 steps of 24 KB at a loaded latency of 2 to 3 us; DRAM at 44 %, the tensor pipe at 24 %
+// (8192 rows of four adapters, rank 64, 4096 + 4096 columns, 39 us).
 constexpr int kAgCols = 256, kAgRows = 32, kAgStages = 4, kAgAtom = kAgRows * 128;      // 64 columns of a stage's rows
 constexpr int kAgVBytes = kAgCols / 64 * kAgAtom, kAgUBytes = 2 * kAgAtom, kAgStage = kAgVBytes + kAgUBytes;
 constexpr int kAgTmem = 256;
