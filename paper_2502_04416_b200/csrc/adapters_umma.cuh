@@ -9,8 +9,8 @@
 // Blocks of a cluster share the columns of both products and exchange the middle's sums, 1 / ctas of the rows each, in rank order.
 //
 // Every operand comes by 16-byte cp.async into 128-byte rows with the 128-byte swizzle: rows of one adapter lie anywhere, widths
-// end inside a block (zeros from there on).  The forward's dropout masks a block
-// of x in shared memory, by the warps that have the epilogue later.  One ring serves both products: blocks of base follow the blocks of x without a gap.
+// end inside a block (zeros from there on).  The forward's dropout masks a block of x in shared memory, by the warps that have the
+// epilogue later.  One ring serves both products: blocks of base follow the blocks of x without a gap.
 #pragma once
 
 #include "adapters.cuh"
