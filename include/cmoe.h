@@ -433,8 +433,8 @@ int64_t cmoe_adapter_scratch_bytes(const cmoe_adapters* ad, int32_t n_rows, int3
  *   row_adapter : device int32 [n_rows], in any order, or NULL: every row takes adapter 0.
  *   z    : device float [n_rows, rank] or NULL; receives A_a xd_t (zeros for rows without an adapter), for the backward pass.
  *   scratch : needed where row_adapter is given and n_rows > 256.
- * Products with fp32 sums (bf16: the narrow middle keeps at least 15 significant bits), rounded once.  A row's result does
- * not depend on the other rows' values.  Asynchronous on `stream`, one launch (two with scratch), allocates nothing;
+ * Products with fp32 sums, rounded once.  In bf16 calls the narrow middle enters the second product with at least 15 significant bits
+ * (off by at most 2^-16 of itself; fp32 calls: in full).  A row's result does not depend on the other rows' values.  Asynchronous on `stream`, one launch (two with scratch), allocates nothing;
  * n_rows == 0 is a no-op.  Two calls that may overlap in time (other streams, captured graphs) need a scratch each.
  * Errors: INVALID_ARG, CAPACITY (scratch too small, n_rows above 2^30), CUDA, UNSUPPORTED. */
 int cmoe_adapter_forward(const cmoe_adapters* ad, const void* x, int64_t ldx, const int32_t* row_adapter, int32_t n_rows,
@@ -448,7 +448,9 @@ int cmoe_adapter_forward(const cmoe_adapters* ad, const void* x, int64_t ldx, co
  *   dx : device, [n_rows, d_in], may be dx_base, or NULL: not wanted.
  *   grad_a [n_adapters, rank, d_in], grad_b [n_adapters, d_out, rank]: device, in the adapters' dtype, 16-byte aligned, written
  *   whole (zeros for adapters without rows), or both NULL: not wanted, then x and z may be NULL.  Sums in fp32 over the rows in
- *   a fixed order: the same call gives the same bits.
+ *   a fixed order: the same call gives the same bits.  In bf16 calls e and z enter the sums with at least 15 significant bits.
+ *   Infinities and NaN in x, dy and z go into the sums of their own adapter as the formulas have them (an e or z whose magnitude is
+ *   below 2^-103 may count as zero beside an infinity).
  * n_rows == 0 zeroes the gradients of the weights.  Scratch is always needed for n_rows > 0.  Otherwise as the forward. */
 int cmoe_adapter_backward(const cmoe_adapters* ad, const void* dy, int64_t ld_dy, const void* x, int64_t ldx, const float* z,
                           const int32_t* row_adapter, int32_t n_rows, const cmoe_dropout_config* drop, const void* dx_base,
