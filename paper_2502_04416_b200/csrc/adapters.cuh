@@ -1301,12 +1301,15 @@ inline int adapter_ctas(long long tiles, int n_sms, int widest, int block, int s
   return c;
 }
 
+// most: the most that any launch of the kernel asks for.  The limit belongs to the kernel and the device, so all host threads share
+// it: it is always set to the same number, and no launch of one thread lowers what another has just asked for.
+template <typename K> inline cudaError_t allow_most_smem(K kernel, size_t smem, size_t most) {
+  return smem > kAdPlainSmem ? cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)most) : cudaSuccess;
+}
 template <typename P>
-inline cudaError_t launch_cluster(bool dep, void (*kernel)(P), dim3 grid, dim3 cluster, size_t smem, cudaStream_t st, const P& args, int threads = kAdThreads) {
-  if (smem > kAdPlainSmem) {
-    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    if (e != cudaSuccess) return e;
-  }
+inline cudaError_t launch_cluster(bool dep, void (*kernel)(P), dim3 grid, dim3 cluster, size_t smem, size_t most, cudaStream_t st, const P& args, int threads = kAdThreads) {
+  const cudaError_t e = allow_most_smem(kernel, smem, most);
+  if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = grid; cfg.blockDim = dim3(threads); cfg.dynamicSmemBytes = smem; cfg.stream = st;
   cudaLaunchAttribute at[2];
@@ -1327,10 +1330,10 @@ inline cudaError_t launch_adapter_tile(const AdapterArgs<bf16>& a, long long til
   using S = AdapterShape<MT, RT, TRANS>;
   const int room = std::max(1, (kAdSmemPerSm / S::kMinBlocks - S::bytes(0)) / S::kRecv);
   const int ctas = adapter_ctas(tiles, n_sms, std::max(a.d_k, a.d_n), 64, room);
-  const size_t smem = S::bytes(ctas);
+  const size_t smem = S::bytes(ctas), most = S::bytes(std::min(room, 8));
   const dim3 grid((unsigned)(tiles * ctas)), cl(ctas);
-  return a.drop.thr16 ? launch_cluster(dep, adapter_kernel<MT, RT, TRANS, true>, grid, cl, smem, st, a)
-                      : launch_cluster(dep, adapter_kernel<MT, RT, TRANS, false>, grid, cl, smem, st, a);
+  return a.drop.thr16 ? launch_cluster(dep, adapter_kernel<MT, RT, TRANS, true>, grid, cl, smem, most, st, a)
+                      : launch_cluster(dep, adapter_kernel<MT, RT, TRANS, false>, grid, cl, smem, most, st, a);
 }
 
 template <int MT, bool TRANS>
@@ -1350,19 +1353,17 @@ inline cudaError_t launch_adapter(const AdapterArgs<bf16>& a, int m, long long t
 template <bool TRANS>
 inline cudaError_t launch_adapter(const AdapterArgs<float>& a, int, long long tiles, int n_sms, bool dep, cudaStream_t st) {
   const int ctas = adapter_ctas(tiles, n_sms, std::max(a.d_k, a.d_n), 32, 8);
-  const size_t smem = AdapterSimtSmem::bytes(ctas);
+  const size_t smem = AdapterSimtSmem::bytes(ctas), most = AdapterSimtSmem::bytes(8);
   const dim3 grid((unsigned)(tiles * ctas)), cl(ctas);
-  return a.drop.thr16 ? launch_cluster(dep, adapter_simt_kernel<TRANS, true>, grid, cl, smem, st, a)
-                      : launch_cluster(dep, adapter_simt_kernel<TRANS, false>, grid, cl, smem, st, a);
+  return a.drop.thr16 ? launch_cluster(dep, adapter_simt_kernel<TRANS, true>, grid, cl, smem, most, st, a)
+                      : launch_cluster(dep, adapter_simt_kernel<TRANS, false>, grid, cl, smem, most, st, a);
 }
 
 template <typename T>
 inline cudaError_t launch_adapter_plan(const AdapterArgs<T>& a, int m, const AdPlanOut& o, cudaStream_t st) {
   const size_t smem = adapter_plan_smem(a.n);
-  if (smem > kAdPlainSmem) {
-    const cudaError_t e = cudaFuncSetAttribute(adapter_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    if (e != cudaSuccess) return e;
-  }
+  const cudaError_t e = allow_most_smem(adapter_plan_kernel, smem, adapter_plan_smem(kAdMaxAdapters));
+  if (e != cudaSuccess) return e;
   int blocks = 1;                              // a batch of 32 rows or two for every warp
   while (blocks < 8 && a.n_rows > blocks * 1024) blocks *= 2;
   cudaLaunchConfig_t cfg = {};
@@ -1395,8 +1396,8 @@ template <int RT> inline cudaError_t launch_outer_rt(OuterArgs p, int n_sms, boo
   const int slices = p.slices[0] + p.slices[1];
   const int ctas = outer_ctas((long long)slices * p.n, n_sms, S::kBlocks, (long long)p.n_rows / p.n / kOutStageRows);
   const dim3 grid(slices, p.n, ctas), cl(1, 1, ctas);
-  return p.drop.thr16 ? launch_cluster(dep, adapter_outer_kernel<RT, true>, grid, cl, S::kSmem, st, p, kOutThreads)
-                      : launch_cluster(dep, adapter_outer_kernel<RT, false>, grid, cl, S::kSmem, st, p, kOutThreads);
+  return p.drop.thr16 ? launch_cluster(dep, adapter_outer_kernel<RT, true>, grid, cl, S::kSmem, S::kSmem, st, p, kOutThreads)
+                      : launch_cluster(dep, adapter_outer_kernel<RT, false>, grid, cl, S::kSmem, S::kSmem, st, p, kOutThreads);
 }
 inline cudaError_t launch_outer(bool bf, const OuterArgs& a, int n_sms, bool dep, cudaStream_t st) {
   if (bf) switch (adapter_rank_tiles(a.r)) {
@@ -1410,8 +1411,8 @@ inline cudaError_t launch_outer(bool bf, const OuterArgs& a, int n_sms, bool dep
   const int slices = p.slices[0] + p.slices[1], chunks = (p.r + kSimtRc - 1) / kSimtRc;
   const int ctas = outer_ctas((long long)slices * p.n * chunks, n_sms, 2, (long long)p.n_rows / p.n / (4 * kAdWarps));
   const dim3 grid(slices, p.n * chunks, ctas), cl(1, 1, ctas);
-  return p.drop.thr16 ? launch_cluster(dep, adapter_outer_simt_kernel<true>, grid, cl, 0, st, p)
-                      : launch_cluster(dep, adapter_outer_simt_kernel<false>, grid, cl, 0, st, p);
+  return p.drop.thr16 ? launch_cluster(dep, adapter_outer_simt_kernel<true>, grid, cl, 0, 0, st, p)
+                      : launch_cluster(dep, adapter_outer_simt_kernel<false>, grid, cl, 0, 0, st, p);
 }
 
 }  // namespace cmoe

@@ -654,8 +654,8 @@ inline cudaError_t launch_adapter_umma(const AdapterArgs<bf16>& a, long long til
   const long long likely = std::min<long long>(tiles, ((long long)a.n_rows + 64LL * (a.n + 1)) / kAuRows + 1);
   const int ctas = adapter_umma_ctas(a.tiles.row_adapter ? likely : tiles, n_sms, (a.d_k + 63) / 64 + (a.d_n + 63) / 64);
   const dim3 grid((unsigned)(tiles * ctas)), cl(ctas);
-  return a.drop.thr16 ? launch_cluster(dep, adapter_umma_kernel<TRANS, true>, grid, cl, kAuSmem, st, a, kAuThreads)
-                      : launch_cluster(dep, adapter_umma_kernel<TRANS, false>, grid, cl, kAuSmem, st, a, kAuThreads);
+  return a.drop.thr16 ? launch_cluster(dep, adapter_umma_kernel<TRANS, true>, grid, cl, kAuSmem, kAuSmem, st, a, kAuThreads)
+                      : launch_cluster(dep, adapter_umma_kernel<TRANS, false>, grid, cl, kAuSmem, kAuSmem, st, a, kAuThreads);
 }
 
 inline cudaError_t launch_outer_umma(OuterArgs p, int n_sms, bool dep, cudaStream_t st) {
@@ -671,8 +671,8 @@ inline cudaError_t launch_outer_umma(OuterArgs p, int n_sms, bool dep, cudaStrea
   // by 1 and 2, 8192 rows of eight adapters, 4096 + 4096: random shares 64, 50, even ones 38, 50).
   while (p.n > 1 && ctas < 8 && 4LL * slices * ctas < 3LL * n_sms && p.n_rows / p.n >= 2048 * ctas) ctas *= 2;
   const dim3 grid(slices, p.n, ctas), cl(1, 1, ctas);
-  return p.drop.thr16 ? launch_cluster(dep, adapter_outer_umma_kernel<true>, grid, cl, kAgSmem, st, p, kAuThreads)
-                      : launch_cluster(dep, adapter_outer_umma_kernel<false>, grid, cl, kAgSmem, st, p, kAuThreads);
+  return p.drop.thr16 ? launch_cluster(dep, adapter_outer_umma_kernel<true>, grid, cl, kAgSmem, kAgSmem, st, p, kAuThreads)
+                      : launch_cluster(dep, adapter_outer_umma_kernel<false>, grid, cl, kAgSmem, kAgSmem, st, p, kAuThreads);
 }
 
 }  // namespace cmoe
