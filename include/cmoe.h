@@ -420,8 +420,9 @@ typedef struct {
   const float* scale;
 } cmoe_adapters;
 
-/* Scratch that the calls below need for n_rows rows (256-byte aligned; contents need not be initialised).  row_adapter
- * given (1) or NULL (0); backward: 1 for cmoe_adapter_backward.  0 for arguments that the calls refuse. */
+/* Scratch that the calls below need for n_rows rows (256-byte aligned; contents need not be initialised); one for n_rows rows serves
+ * any smaller batch of the same adapters too.  row_adapter given (1) or NULL (0); backward: 1 for cmoe_adapter_backward.  0 for
+ * arguments that the calls refuse, and where none is needed. */
 int64_t cmoe_adapter_scratch_bytes(const cmoe_adapters* ad, int32_t n_rows, int32_t with_row_adapter, int32_t backward);
 
 /* out_t = base_t + s_a B_a (A_a xd_t) for every row t with its own adapter a = row_adapter[t]; a number outside

@@ -1260,11 +1260,12 @@ inline long long adapter_max_tiles(long long n_rows, int n, int m, bool one) {
   return one ? (n_rows + m - 1) / m : n_rows / m + std::min<long long>(n + 1, n_rows);
 }
 
-// The layout serves every tile height of the devices, so that its size does not depend on the one in use.
+// A scratch for some rows serves any fewer, whatever tiles those take: room for as many tiles as the lowest have, and for the places of
+// the highest that the batch can take (a longer batch never has fewer of them).
 struct AdapterScratch { size_t tile_start, tile_adapter, row_list, u_e, u_z, total; };
 inline AdapterScratch adapter_scratch(bool bf, int n_rows, int n, int r, bool backward, bool one, bool tall) {
   AdapterScratch s{};
-  const int m_lo = tall ? kAdTallRows : bf ? 16 : kSimtM, m_hi = tall ? kAdTallRows : kSimtM;
+  const int m_lo = bf ? 16 : kSimtM, m_hi = tall ? kAdTallRows : kSimtM;
   const size_t tiles = (size_t)adapter_max_tiles(n_rows, n, m_lo, one), places = (size_t)adapter_max_tiles(n_rows, n, m_hi, one) * m_hi;
   size_t at = 0;
   const auto take = [&](size_t bytes) { const size_t p = at; at += (bytes + 255) / 256 * 256; return p; };
