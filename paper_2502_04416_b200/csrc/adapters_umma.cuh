@@ -11,6 +11,10 @@
 // Every operand comes by 16-byte cp.async into 128-byte rows with the 128-byte swizzle: rows of one adapter lie anywhere, widths
 // end inside a block (zeros from there on).  The forward's dropout masks a block of x in shared memory, by the warps that have the
 // epilogue later.  One ring serves both products: blocks of base follow the blocks of x without a gap.
+//
+// A kernel that follows may allocate tensor memory before it waits for these (a layer's first kernel does, chained to whatever precedes
+// it).  It becomes resident only once every block here has let it, which a block does when it has its own: otherwise the two could wait
+// for each other, the one for tensor memory and the other for the end of this grid.
 #pragma once
 
 #include "adapters.cuh"
@@ -85,7 +89,6 @@ adapter_umma_kernel(const AdapterArgs<bf16> p) {
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
   grid_dep_wait();
-  grid_dep_trigger();
   const int tile = blockIdx.x / ctas;
   int a = 0;
   if (p.tiles.row_adapter) {
@@ -107,6 +110,7 @@ adapter_umma_kernel(const AdapterArgs<bf16> p) {
   }
   tc_fence_before();
   __syncthreads();
+  grid_dep_trigger();                                                          // this block has its tensor memory (see the header)
   rc_cluster_arrive();
   rc_cluster_wait();                                                           // every peer's barriers are there
   tc_fence_after();
@@ -445,13 +449,13 @@ adapter_outer_umma_kernel(const OuterArgs p) {
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
   grid_dep_wait();                                         // before the allocation: a block that waits holds no tensor memory
-  grid_dep_trigger();
   if (warp == kAuEpiWarps + kAuLoadWarps) {
     tmem_alloc(smem_u32(tmem_slot), kAgTmem);
     tmem_relinquish();
   }
   tc_fence_before();
   __syncthreads();
+  grid_dep_trigger();                                      // this block has its tensor memory
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
   int side, slice;
