@@ -823,10 +823,9 @@ adapter_outer_kernel(const OuterArgs p) {
       return n >= mine || pos >= hi ? -1 : p.tiles.row_adapter ? __ldcg(p.tiles.row_list + pos) : (int)pos;
     };
     int row = row_of(0), n = 0;
-    bool ok = true;
     for (; n < mine; ++n) {
       const int s = n % kDepth, use = n / kDepth, next = row_of(n + 1);
-      if (use > 0 && !mbar_wait_warp(empty0 + 8 * s, (use - 1) & 1, abort_flag, &g_adapter_error, kErrWaitEmpty)) { ok = false; break; }
+      if (use > 0 && !mbar_wait_warp(empty0 + 8 * s, (use - 1) & 1, abort_flag, &g_adapter_error, kErrWaitEmpty)) break;
       const uint32_t dst = smem_u32(smem) + s * S::kStage, bar = full0 + 8 * s;
       // 16-row tiles of the stage that U has: the last stage may end early
       const long long t0 = (lo + ((long long)n * ctas + rank) * kOutStageRows) / 16;
@@ -840,11 +839,12 @@ adapter_outer_kernel(const OuterArgs p) {
       if (half == 0 && elect_one()) bulk_copy(dst + S::kV, (const uint4*)sd.u + t0 * RT * 32, u_tiles * RT * 512, bar);
       row = next;
     }
-    if (!ok)                                               // a wait ran out: what is on its way lands before the block ends
-      for (int i = max(0, n - kDepth); i < n; ++i) {
-        const long long t = clock64();
-        while (!mbar_try_wait(full0 + 8 * (i % kDepth), (i / kDepth) & 1) && clock64() - t < kUmmaWaitCycles) {}
-      }
+    // What is on its way lands before the ring becomes the sums' memory and before the block ends, also where a wait ran out, here or
+    // in a warp of the products (otherwise those have waited for it all).
+    for (int i = max(0, n - kDepth); i < n; ++i) {
+      const long long t = clock64();
+      while (!mbar_try_wait(full0 + 8 * (i % kDepth), (i / kDepth) & 1) && clock64() - t < kUmmaWaitCycles) {}
+    }
   } else {
     // ---- products: two steps of 16 rows a stage
     for (int n = 0; n < mine; ++n) {
