@@ -431,7 +431,7 @@ int64_t cmoe_adapter_scratch_bytes(const cmoe_adapters* ad, int32_t n_rows, int3
  *          shared projection gave for the rows;  out : device, [n_rows, d_out], row stride ld_out; may be base (same pointer
  *          and stride), overlaps neither x nor base otherwise.  Strides in elements, at least the width, at most 2^28; pointers and
  *          strides are multiples of 16 bytes.  Rows of other matrices may lie between (column slices of a wider one).
- *   row_adapter : device int32 [n_rows], in any order, or NULL: every row takes adapter 0.
+ *   row_adapter : device int32 [n_rows], 4-byte aligned, in any order, or NULL: every row takes adapter 0.
  *   z    : device float [n_rows, rank] or NULL; receives A_a xd_t (zeros for rows without an adapter), for the backward pass.
  *   scratch : needed where row_adapter is given and n_rows > 256.
  * Products with fp32 sums, rounded once.  In bf16 calls the narrow middle enters the second product with at least 15 significant bits

@@ -1463,6 +1463,7 @@ int plan_adapter_pass(AdapterPass<T>& p, const cmoe_adapters* ad, const int32_t*
   p.tall = adapter_tall(bf, n_rows, ad->n_adapters, ad->rank, p.small);
   const bool planned = row_adapter && !p.small;
   const AdapterScratch lay = adapter_scratch(bf, n_rows, ad->n_adapters, ad->rank, backward, !planned, p.tall);
+  if ((uintptr_t)row_adapter & 3) return arg_fail(CMOE_ERR_INVALID_ARG, "adapters: row_adapter not 4-byte aligned");
   if (lay.total > 0) {
     if (!scratch || ((uintptr_t)scratch & 255)) return arg_fail(CMOE_ERR_INVALID_ARG, "adapters: scratch null or not 256-byte aligned");
     if (scratch_bytes < (int64_t)lay.total) return arg_fail(CMOE_ERR_CAPACITY, "adapters: scratch too small");
