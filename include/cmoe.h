@@ -437,6 +437,7 @@ int64_t cmoe_adapter_scratch_bytes(const cmoe_adapters* ad, int32_t n_rows, int3
  * Products with fp32 sums, rounded once.  In bf16 calls the narrow middle enters the second product with at least 15 significant bits
  * (off by at most 2^-16 of itself; fp32 calls: in full).  A row's result does not depend on the other rows' values.  Asynchronous on `stream`, one launch (two with scratch), allocates nothing;
  * n_rows == 0 is a no-op.  Two calls that may overlap in time (other streams, captured graphs) need a scratch each.
+ * z and the scratch in use overlap nothing else of the call; out overlaps none of the set's arrays.
  * Errors: INVALID_ARG, CAPACITY (scratch too small, n_rows above 2^30), CUDA, UNSUPPORTED. */
 int cmoe_adapter_forward(const cmoe_adapters* ad, const void* x, int64_t ldx, const int32_t* row_adapter, int32_t n_rows,
                          const cmoe_dropout_config* drop, const void* base, int64_t ld_base, void* out, int64_t ld_out, float* z,
@@ -452,7 +453,8 @@ int cmoe_adapter_forward(const cmoe_adapters* ad, const void* x, int64_t ldx, co
  *   a fixed order: the same call gives the same bits.  In bf16 calls e and z enter the sums with at least 15 significant bits.
  *   Infinities and NaN in x, dy and z go into the sums of their own adapter as the formulas have them (an e or z whose magnitude is
  *   below 2^-103 may count as zero beside an infinity).
- * n_rows == 0 zeroes the gradients of the weights.  Scratch is always needed for n_rows > 0.  Otherwise as the forward. */
+ * n_rows == 0 zeroes the gradients of the weights.  Scratch is always needed for n_rows > 0; it, grad_a and grad_b overlap nothing else
+ * of the call, dx overlaps none of dy, x, z and the set's arrays (x and z count where they are read).  Otherwise as the forward. */
 int cmoe_adapter_backward(const cmoe_adapters* ad, const void* dy, int64_t ld_dy, const void* x, int64_t ldx, const float* z,
                           const int32_t* row_adapter, int32_t n_rows, const cmoe_dropout_config* drop, const void* dx_base,
                           int64_t ld_dx_base, void* dx, int64_t ld_dx, void* grad_a, void* grad_b, void* scratch,

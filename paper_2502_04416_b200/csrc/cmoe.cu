@@ -1401,6 +1401,35 @@ bool overlap(const Mat& a, const Mat& b, int64_t rows, int64_t esz) {
 }
 bool same(const Mat& a, const Mat& b) { return a.p == b.p && a.ld == b.ld; }
 
+// Memory that a call reads or writes: rows of a matrix, or one run of bytes (a single row).
+struct Piece { const char* what; Mat m; int64_t rows, esz; };
+Piece run_of(const char* what, const void* p, int64_t bytes) { return {what, {p, bytes, bytes}, 1, 1}; }
+
+bool meet(const Piece& a, const Piece& b) {
+  if (!a.m.p || !b.m.p || a.rows <= 0 || b.rows <= 0 || a.m.cols <= 0 || b.m.cols <= 0) return false;
+  if (a.rows > 1 && b.rows > 1) return a.esz != b.esz || a.rows != b.rows || overlap(a.m, b.m, a.rows, a.esz);
+  const Piece &run = a.rows == 1 ? a : b, &mat = a.rows == 1 ? b : a;
+  const auto lo = (intptr_t)run.m.p, hi = lo + (intptr_t)(run.m.cols * run.esz), p = (intptr_t)mat.m.p;
+  const int64_t line = mat.m.ld * mat.esz, width = mat.m.cols * mat.esz;
+  const int64_t row = lo < p + width ? 0 : (lo - p - width) / line + 1;        // the first that ends behind the run's start
+  return row < mat.rows && p + row * line < hi;
+}
+
+// Refuses a piece that is written and shares memory with one that is read or with another that is written.
+template <size_t W, size_t R> int check_apart(const Piece (&written)[W], const Piece (&read)[R]) {
+  const auto refuse = [](const Piece& a, const Piece& b) {
+    snprintf(g_last_error, sizeof(g_last_error), "adapters: %s and %s overlap", a.what, b.what);
+    return CMOE_ERR_INVALID_ARG;
+  };
+  for (size_t i = 0; i < W; ++i) {
+    for (size_t j = i + 1; j < W; ++j)
+      if (meet(written[i], written[j])) return refuse(written[i], written[j]);
+    for (const Piece& r : read)
+      if (meet(written[i], r)) return refuse(written[i], r);
+  }
+  return CMOE_OK;
+}
+
 int check_drop(const cmoe_dropout_config* d, int64_t rows, Drop* out) {
   *out = Drop{};
   if (!d) return CMOE_OK;
@@ -1449,25 +1478,34 @@ bool wide_rows(const Mat& m, int64_t width) { return !m.p || (((uintptr_t)m.p & 
 // What both directions share once the arguments are known to be good.
 template <typename T> struct AdapterPass {
   AdapterArgs<T> a{};
+  AdapterScratch lay{};
   AdPlanOut plan{};
   bool small = false, tall = false;
   int m = 0, n_sms = 0;
   long long tiles = 0;
 };
 
+// The tiles' form and the scratch that it needs.
 template <typename T>
-int plan_adapter_pass(AdapterPass<T>& p, const cmoe_adapters* ad, const int32_t* row_adapter, int32_t n_rows, bool backward,
-                      void* scratch, int64_t scratch_bytes) {
+int check_adapter_scratch(AdapterPass<T>& p, const cmoe_adapters* ad, const int32_t* row_adapter, int32_t n_rows, bool backward,
+                          void* scratch, int64_t scratch_bytes) {
   constexpr bool bf = sizeof(T) == 2;
   p.small = adapter_small(row_adapter, n_rows, backward);
   p.tall = adapter_tall(bf, n_rows, ad->n_adapters, ad->rank, p.small);
-  const bool planned = row_adapter && !p.small;
-  const AdapterScratch lay = adapter_scratch(bf, n_rows, ad->n_adapters, ad->rank, backward, !planned, p.tall);
+  p.lay = adapter_scratch(bf, n_rows, ad->n_adapters, ad->rank, backward, !row_adapter || p.small, p.tall);
   if ((uintptr_t)row_adapter & 3) return arg_fail(CMOE_ERR_INVALID_ARG, "adapters: row_adapter not 4-byte aligned");
-  if (lay.total > 0) {
+  if (p.lay.total > 0) {
     if (!scratch || ((uintptr_t)scratch & 255)) return arg_fail(CMOE_ERR_INVALID_ARG, "adapters: scratch null or not 256-byte aligned");
-    if (scratch_bytes < (int64_t)lay.total) return arg_fail(CMOE_ERR_CAPACITY, "adapters: scratch too small");
+    if (scratch_bytes < (int64_t)p.lay.total) return arg_fail(CMOE_ERR_CAPACITY, "adapters: scratch too small");
   }
+  return CMOE_OK;
+}
+
+template <typename T>
+int plan_adapter_pass(AdapterPass<T>& p, const cmoe_adapters* ad, const int32_t* row_adapter, int32_t n_rows, bool backward, void* scratch) {
+  constexpr bool bf = sizeof(T) == 2;
+  const bool planned = row_adapter && !p.small;
+  const AdapterScratch& lay = p.lay;
   RC_TRY(device_sms(&p.n_sms));
   p.m = adapter_tile_rows(bf, n_rows, p.small, p.tall, p.n_sms);
   char* s = static_cast<char*>(scratch);
@@ -1523,11 +1561,37 @@ int check_adapter_forward(const cmoe_adapters* ad, const Mat& x, int32_t n_rows,
   return CMOE_OK;
 }
 
+// What the set of adapters and its rows' numbers take.
+struct AdapterPieces {
+  Piece ids, a, b, scale;
+  AdapterPieces(const cmoe_adapters* ad, const int32_t* row_adapter, int64_t n_rows)
+      : ids(run_of("row_adapter", row_adapter, n_rows * 4)), a(weights("a", ad, ad->a, ad->d_in)), b(weights("b", ad, ad->b, ad->d_out)),
+        scale(run_of("scale", ad->scale, (int64_t)ad->n_adapters * 4)) {}
+  static Piece weights(const char* what, const cmoe_adapters* ad, const void* p, int64_t width) {
+    return run_of(what, p, (int64_t)ad->n_adapters * ad->rank * width * (ad->dtype == CMOE_BF16 ? 2 : 4));
+  }
+};
+
+// All that does not need the device; the matrices' own overlaps are check_adapter_forward's.
+template <typename T>
+int check_adapter_forward_pass(AdapterPass<T>& p, const cmoe_adapters* ad, const Mat& x, const int32_t* row_adapter, int32_t n_rows, const Mat& base,
+                               const Mat& out, float* z, void* scratch, int64_t scratch_bytes) {
+  RC_TRY(check_adapter_scratch(p, ad, row_adapter, n_rows, false, scratch, scratch_bytes));
+  const AdapterPieces s(ad, row_adapter, n_rows);
+  const Piece mo{"out", out, n_rows, sizeof(T)};
+  const Piece written[] = {run_of("z", z, (int64_t)n_rows * ad->rank * 4), run_of("scratch", scratch, (int64_t)p.lay.total)};
+  const Piece read[] = {{"x", x, n_rows, sizeof(T)}, {"base", base, n_rows, sizeof(T)}, mo, s.ids, s.a, s.b, s.scale};
+  RC_TRY(check_apart(written, read));
+  const Piece result[] = {mo}, set[] = {s.ids, s.a, s.b, s.scale};
+  return check_apart(result, set);
+}
+
 template <typename T>
 int adapter_forward_impl(const cmoe_adapters* ad, const Mat& x, const int32_t* row_adapter, int32_t n_rows, const Drop& drop, const Mat& base,
                          const Mat& out, float* z, void* scratch, int64_t scratch_bytes, cudaStream_t st) {
   AdapterPass<T> p;
-  RC_TRY(plan_adapter_pass(p, ad, row_adapter, n_rows, false, scratch, scratch_bytes));
+  RC_TRY(check_adapter_forward_pass(p, ad, x, row_adapter, n_rows, base, out, z, scratch, scratch_bytes));
+  RC_TRY(plan_adapter_pass(p, ad, row_adapter, n_rows, false, scratch));
   return adapter_forward_launch(ad, p, x, base, out, z, drop, st);
 }
 
@@ -1536,7 +1600,19 @@ int adapter_backward_impl(const cmoe_adapters* ad, const Mat& dy, const Mat& x, 
                           const Drop& drop, const Mat& dx_base, const Mat& dx, void* grad_a, void* grad_b, void* scratch,
                           int64_t scratch_bytes, cudaStream_t st) {
   AdapterPass<T> p;
-  RC_TRY(plan_adapter_pass(p, ad, row_adapter, n_rows, true, scratch, scratch_bytes));
+  RC_TRY(check_adapter_scratch(p, ad, row_adapter, n_rows, true, scratch, scratch_bytes));
+  {
+    const AdapterPieces s(ad, row_adapter, n_rows);
+    const Piece mdx{"dx", dx, n_rows, sizeof(T)}, mz = run_of("z", grad_a ? z : nullptr, (int64_t)n_rows * ad->rank * 4);
+    const Piece written[] = {AdapterPieces::weights("grad_a", ad, grad_a, ad->d_in), AdapterPieces::weights("grad_b", ad, grad_b, ad->d_out),
+                             run_of("scratch", scratch, (int64_t)p.lay.total)};
+    const Piece read[] = {{"dy", dy, n_rows, sizeof(T)}, {"x", {grad_a ? x.p : nullptr, x.ld, x.cols}, n_rows, sizeof(T)},
+                          {"dx_base", dx_base, n_rows, sizeof(T)}, mdx, mz, s.ids, s.a, s.b, s.scale};
+    RC_TRY(check_apart(written, read));
+    const Piece result[] = {mdx}, set[] = {mz, s.ids, s.a, s.b, s.scale};
+    RC_TRY(check_apart(result, set));
+  }
+  RC_TRY(plan_adapter_pass(p, ad, row_adapter, n_rows, true, scratch));
   p.a.x = (const T*)dy.p; p.a.ldx = dy.ld;
   p.a.w1 = (const T*)ad->b; p.a.w2 = (const T*)ad->a;
   p.a.base = (const T*)dx_base.p; p.a.ld_base = dx_base.ld;
@@ -1678,7 +1754,8 @@ int cmoe_ffn_forward_adapted(cmoe_layer* L, const void* x, int32_t T, const cmoe
   RC_TRY(check_adapter_forward(ad, mx, T, mo, mo, nullptr));
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const auto go = [&](auto pass) -> int {
-    RC_TRY(plan_adapter_pass(pass, ad, row_adapter, T, false, scratch, scratch_bytes));
+    RC_TRY(check_adapter_forward_pass(pass, ad, mx, row_adapter, T, mo, mo, nullptr, scratch, scratch_bytes));
+    RC_TRY(plan_adapter_pass(pass, ad, row_adapter, T, false, scratch));
     RC_TRY(cmoe_ffn_forward(L, x, T, out, stream));
     RC_TRY(adapter_forward_launch(ad, pass, mx, mo, mo, nullptr, Drop{}, st));
     L->launches += pass.plan.row_list ? 2 : 1;

@@ -39,3 +39,66 @@ def test_row_numbers_off_their_boundary(lib, rows, by):
     """A misaligned address would fault on the device."""
     assert _fwd(lib, rows, ids=AT["ids"] + by) == -1 and b"row_adapter" in lib.cmoe_last_error()
     assert _bwd(lib, rows, ids=AT["ids"] + by) == -1 and b"row_adapter" in lib.cmoe_last_error()
+
+
+# ------------------------------------------------------------------ overlaps
+BYTES = dict(dy=ROWS * D_OUT * 2, x=ROWS * D_IN * 2, z=ROWS * R * 4, base=ROWS * D_IN * 2, out=ROWS * D_IN * 2, ids=ROWS * 4, a=N * R * D_IN * 2,
+             b=N * R * D_OUT * 2, scale=N * 4, ga=N * R * D_IN * 2, gb=N * R * D_OUT * 2, scratch=1 << 16)
+
+
+def _apart(lib, call, moved, to):
+    """Whether the call takes `moved` at the end of `to` and refuses it one boundary earlier.  A call that is taken would be launched, so
+    that is asked of one which is refused later, for a scratch that is named last."""
+    size = dict(BYTES, base=ROWS * D_OUT * 2, out=ROWS * D_OUT * 2) if call is _fwd else BYTES
+    step = 256 if moved == "scratch" else 16
+    inside = AT[to] + (size[to] - 1) // step * step
+    assert call(lib, **{moved: inside}) == -1, (moved, to)
+    text = lib.cmoe_last_error().decode()
+    assert "overlap" in text, text
+    return text
+
+
+@pytest.mark.parametrize("moved,others", [("z", ("x", "base", "out", "ids", "a", "b", "scale")),
+                                          ("scratch", ("x", "base", "out", "ids", "a", "b", "scale", "z")),
+                                          ("out", ("ids", "a", "b", "scale"))])
+def test_forward_overlaps(lib, moved, others):
+    for to in others:
+        text = _apart(lib, _fwd, moved, to)
+        assert {"ids": "row_adapter"}.get(to, to) in text and moved in text
+
+
+@pytest.mark.parametrize("moved,others", [("ga", ("dy", "x", "z", "base", "out", "ids", "a", "b", "scale", "gb")),
+                                          ("gb", ("dy", "x", "z", "base", "out", "ids", "a", "b", "scale", "ga")),
+                                          ("scratch", ("dy", "x", "z", "base", "out", "ids", "a", "b", "scale", "ga", "gb")),
+                                          ("out", ("z", "ids", "a", "b", "scale"))])
+def test_backward_overlaps(lib, moved, others):
+    names = dict(ids="row_adapter", ga="grad_a", gb="grad_b", base="dx_base", out="dx")
+    for to in others:
+        text = _apart(lib, _bwd, moved, to)
+        assert names.get(to, to) in text and names.get(moved, moved) in text
+
+
+def test_what_only_lies_side_by_side_does_not_overlap(lib):
+    """z, a run of bytes, in the gap between a matrix's rows or behind its last one; the call is then refused for the overlap that the
+    scratch has with a, which is looked at later."""
+    def says(**kw):
+        assert _fwd(lib, **{**dict(scratch=AT["a"]), **kw}) == -1
+        return lib.cmoe_last_error().decode()
+    size = ROWS * R * 4
+    ld = size // 2 + 64 + D_IN                              # in elements of two bytes: rows with a gap that z fits in
+    assert "scratch and a" in says()
+    assert "scratch and a" in says(ld=dict(x=ld), z=AT["x"] + D_IN * 2)
+    assert "z and x" in says(ld=dict(x=ld), z=AT["x"] + D_IN * 2 - 16)
+    assert "z and x" in says(ld=dict(x=ld), z=AT["x"] + ld * 2 - size + 16)
+    assert "scratch and a" in says(z=AT["x"] + ROWS * D_IN * 2)
+    assert "z and x" in says(z=AT["x"] + ROWS * D_IN * 2 - 16)
+    assert "z and x" in says(z=AT["x"] - size + 16)
+    assert "scratch and a" in says(z=AT["x"] - size)
+
+
+def test_what_is_not_read_may_lie_anywhere(lib):
+    """Without the weights' gradients x and z are not looked at; with the gradients they are."""
+    bad = dict(scratch=AT["a"])
+    assert _bwd(lib, ga=None, gb=None, x=AT["out"], z=AT["out"], **bad) == -1 and b"scratch and a" in lib.cmoe_last_error()
+    assert _bwd(lib, z=AT["out"], **bad) == -1 and b"scratch and a" in lib.cmoe_last_error()
+    assert _bwd(lib, z=AT["out"]) == -1 and b"dx and z" in lib.cmoe_last_error()
