@@ -410,7 +410,7 @@ int cmoe_dropout(const void* x, int64_t ldx, const void* residual, int64_t ld_re
 
 /* A set of low-rank adapters of one projection [d_in] -> [d_out].
  *   a : device, [n_adapters, rank, d_in]; b : device, [n_adapters, d_out, rank]; both contiguous, 16-byte aligned, of dtype.
- *   scale : device float [n_adapters] (alpha / rank of each) or NULL (1).
+ *   scale : device float [n_adapters], 8-byte aligned (alpha / rank of each), or NULL (1).
  *   1 <= n_adapters <= 1024; rank a multiple of 8, at most 64 (adapters of other ranks are padded with zeros, which
  *   changes no result); d_in, d_out multiples of 8, at most 2^24.  Weights are taken to be finite.
  * The struct is read during the call; the arrays belong to the caller. */
@@ -432,7 +432,7 @@ int64_t cmoe_adapter_scratch_bytes(const cmoe_adapters* ad, int32_t n_rows, int3
  *          and stride), overlaps neither x nor base otherwise.  Strides in elements, at least the width, at most 2^28; pointers and
  *          strides are multiples of 16 bytes.  Rows of other matrices may lie between (column slices of a wider one).
  *   row_adapter : device int32 [n_rows], 4-byte aligned, in any order, or NULL: every row takes adapter 0.
- *   z    : device float [n_rows, rank] or NULL; receives A_a xd_t (zeros for rows without an adapter), for the backward pass.
+ *   z    : device float [n_rows, rank], 8-byte aligned, or NULL; receives A_a xd_t (zeros for rows without an adapter), for the backward pass.
  *   scratch : needed where row_adapter is given and n_rows > 256.
  * Products with fp32 sums, rounded once.  In bf16 calls the narrow middle enters the second product with at least 15 significant bits
  * (off by at most 2^-16 of itself; fp32 calls: in full).  A row's result does not depend on the other rows' values.  Asynchronous on `stream`, one launch (two with scratch), allocates nothing;

@@ -541,8 +541,13 @@ def _adapters(dtype, dev: int, a, b, scale) -> CmoeAdapters:
     code = CMOE_BF16 if dtype is _torch.bfloat16 else CMOE_FP32 if dtype is _torch.float32 else None
     if code is None:
         raise TypeError(f"unsupported dtype {dtype}")
-    return CmoeAdapters(n, r, d_in, d_out, code, _like(a, "a", (n, r, d_in), dtype, dev), _like(b, "b", (n, d_out, r), dtype, dev),
-                        None if scale is None else _like(scale, "scale", (n,), _torch.float32, dev))
+    s_ptr = None if scale is None else _like(scale, "scale", (n,), _torch.float32, dev)
+    if s_ptr is not None and s_ptr & 7:                        # a slice of a larger set may start anywhere: the call takes it on 8 bytes
+        scale = scale.clone()
+        s_ptr = scale.data_ptr()
+    ad = CmoeAdapters(n, r, d_in, d_out, code, _like(a, "a", (n, r, d_in), dtype, dev), _like(b, "b", (n, d_out, r), dtype, dev), s_ptr)
+    ad.scale_tensor = scale                                    # lives as long as the struct that has its address
+    return ad
 
 
 ADAPTER_SMALL_ROWS = 256     # row counts up to which cmoe_adapter_forward needs no scratch
