@@ -477,12 +477,17 @@ def _matrix(t, what: str, rows: int, cols: int, dtype, dev: int) -> int:
     return stride[0] if rows > 1 else cols                     # the stride of a single row has no meaning
 
 
+_MOST = 2**31 - 1     # counts are passed in 32 bits, and ctypes takes larger ones modulo 2^32
+
+
 def _rows(t, what: str):
     """(rows, columns, row stride, type, device) of a row-strided CUDA matrix."""
     dev = t.get_device()
     if dev < 0 or t.dim() != 2:
         raise ValueError(f"{what}: a two-dimensional CUDA tensor is expected")
     rows, cols = t.shape
+    if rows > _MOST or cols > _MOST:
+        raise ValueError(f"{what}: more than {_MOST} rows or columns")
     dtype = t.dtype
     return rows, cols, _matrix(t, what, rows, cols, dtype, dev), dtype, dev
 
@@ -538,6 +543,8 @@ def dropout(x, drop: Dropout, residual=None, out=None, stream=None):
 def _adapters(dtype, dev: int, a, b, scale) -> CmoeAdapters:
     n, r, d_in = a.shape
     d_out = b.shape[1]
+    if max(n, r, d_in, d_out) > _MOST:
+        raise ValueError(f"a, b: a dimension above {_MOST}")
     code = CMOE_BF16 if dtype is _torch.bfloat16 else CMOE_FP32 if dtype is _torch.float32 else None
     if code is None:
         raise TypeError(f"unsupported dtype {dtype}")
