@@ -1647,8 +1647,8 @@ int cmoe_dropout(const void* x, int64_t ldx, const void* residual, int64_t ld_re
   const int64_t esz = dtype == CMOE_BF16 ? 2 : 4;
   const Mat mx{x, ldx, cols}, mr{residual, ld_residual, cols}, mo{out, ld_out, cols};
   for (const Mat* m : {&mx, &mr, &mo})
-    if (m->p && (m->ld < cols || m->ld > (1LL << 40) || (uintptr_t)m->p % esz))
-      return arg_fail(CMOE_ERR_INVALID_ARG, "dropout: a row stride below the width, or a pointer that is not element-aligned");
+    if (m->p && (m->ld < cols || m->ld > (1LL << 40) || (uintptr_t)m->p % esz || m->ld * esz > (1LL << 60) / rows))   // no product wraps
+      return arg_fail(CMOE_ERR_INVALID_ARG, "dropout: a row stride below the width or beyond all memory, or a pointer that is not element-aligned");
   if (!same(mx, mo) && overlap(mx, mo, rows, esz)) return arg_fail(CMOE_ERR_INVALID_ARG, "dropout: x and out overlap without being the same");
   if (residual && !same(mr, mo) && overlap(mr, mo, rows, esz))
     return arg_fail(CMOE_ERR_INVALID_ARG, "dropout: residual and out overlap without being the same");

@@ -102,3 +102,14 @@ def test_what_is_not_read_may_lie_anywhere(lib):
     assert _bwd(lib, ga=None, gb=None, x=AT["out"], z=AT["out"], **bad) == -1 and b"scratch and a" in lib.cmoe_last_error()
     assert _bwd(lib, z=AT["out"], **bad) == -1 and b"scratch and a" in lib.cmoe_last_error()
     assert _bwd(lib, z=AT["out"]) == -1 and b"dx and z" in lib.cmoe_last_error()
+
+
+@pytest.mark.parametrize("what", ["x", "residual", "out"])
+@pytest.mark.parametrize("rows,ld", [(2**31 - 1, 2**40), (2**30, 2**31), (2**25, 2**36)])
+def test_dropout_of_more_than_all_memory(lib, what, rows, ld):
+    """Products of rows and strides that pass 64 bits, or come near: the check for overlaps counts with them."""
+    lds = {**dict(x=10, residual=10, out=10), what: ld}
+    drop = binding.CmoeDropoutConfig(0.1, 1, 0, 0)
+    at = dict(x=1 << 44, residual=1 << 45, out=1 << 46)
+    assert lib.cmoe_dropout(at["x"], lds["x"], at["residual"], lds["residual"], rows, 10, 1, C.byref(drop), at["out"], lds["out"], None) == -1
+    assert b"stride" in lib.cmoe_last_error()
