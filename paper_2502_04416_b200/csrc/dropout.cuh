@@ -76,7 +76,7 @@ template <typename T> struct DropoutArgs {
 template <typename T>
 __global__ void __launch_bounds__(kDropThreads)
 dropout_kernel(const DropoutArgs<T> p) {
-  const unsigned nb = (unsigned)(p.cols + 7) >> 3;
+  const unsigned nb = ((unsigned)p.cols + 7u) >> 3;
   const unsigned long long total = (unsigned long long)p.rows * nb;
   const unsigned long long stride = (unsigned long long)gridDim.x * kDropThreads;
   unsigned long long i = (unsigned long long)blockIdx.x * kDropThreads + threadIdx.x;
@@ -187,7 +187,7 @@ dropout_flat_kernel(const DropoutArgs<T> p) {
 template <typename T>
 __global__ void __launch_bounds__(kDropThreads)
 dropout_ragged_kernel(const DropoutArgs<T> p) {
-  const unsigned nb = (unsigned)(p.cols + 7) >> 3;
+  const unsigned nb = ((unsigned)p.cols + 7u) >> 3;
   const unsigned long long total = (unsigned long long)p.rows * nb;
   const unsigned long long stride = (unsigned long long)gridDim.x * kDropThreads;
   const unsigned lane = threadIdx.x & 31;
@@ -226,7 +226,7 @@ inline int drop_grid(unsigned long long blocks8, int n_sms) {
 }
 
 template <typename T> inline cudaError_t launch_dropout(const DropoutArgs<T>& a, int n_sms, cudaStream_t st) {
-  const int grid = drop_grid((unsigned long long)a.rows * ((a.cols + 7) / 8), n_sms);
+  const int grid = drop_grid((unsigned long long)a.rows * (((unsigned)a.cols + 7u) / 8), n_sms);
   const auto on16 = [](const void* q, long long ld) { return ((uintptr_t)q & 15) == 0 && (ld * sizeof(T)) % 16 == 0; };
   if (on16(a.x, a.ldx) && on16(a.out, a.ld_out) && (!a.residual || on16(a.residual, a.ld_res)))
     return launch_kernel(false, dropout_kernel<T>, dim3(grid), dim3(kDropThreads), 0, st, a);
