@@ -462,8 +462,14 @@ int cmoe_adapter_backward(const cmoe_adapters* ad, const void* dy, int64_t ld_dy
 
 /* Device-side error word of this device's adapter calls (all that are declared above and below): 0, or a code written by a kernel
  * whose bounded wait inside its block or cluster ran out (the outputs of that call are undefined).  Synchronises `stream`.
- * Returns CMOE_ERR_DEVICE_TIMEOUT when the word is non-zero; it is reported once and cleared.  device_error_word may be NULL.  Errors: CUDA. */
+ * Returns CMOE_ERR_DEVICE_TIMEOUT when the word is non-zero; it is reported once and cleared, whichever stream or thread made the call that
+ * it comes from (that call itself returned CMOE_OK when it was enqueued).  device_error_word may be NULL.  Errors: CUDA. */
 int cmoe_adapter_status(int32_t* device_error_word, void* stream);
+
+/* Self-test of the give-up path, as cmoe_layer_selftest_wait_timeout: one warp waits, for limit_cycles SM clock cycles (1e3 .. 2e9), on
+ * a barrier that nobody arrives on, through the bounded wait of the adapters' kernels, and returns normally with its code in this device's error
+ * word, which cmoe_adapter_status then reports.  Asynchronous on `stream`.  Errors: INVALID_ARG, CUDA, UNSUPPORTED. */
+int cmoe_adapter_selftest_wait_timeout(int64_t limit_cycles, void* stream);
 
 /* out_t = F_MoE(x_t) + s_a B_a A_a x_t: cmoe_ffn_forward with an adapter per request beside the layer, which all of them share.
  * The adapters' d_in and d_out are the layer's d_model and their dtype is the layer's; x, T, out as in cmoe_ffn_forward,

@@ -28,7 +28,7 @@ EXPORTS = [
     "cmoe_layer_destroy", "cmoe_token_permute_scratch_bytes",
     "cmoe_token_permute", "cmoe_token_permute_static", "cmoe_status_string", "cmoe_last_error",
     "cmoe_dropout", "cmoe_adapter_scratch_bytes", "cmoe_adapter_forward", "cmoe_adapter_backward", "cmoe_adapter_status",
-    "cmoe_ffn_forward_adapted",
+    "cmoe_adapter_selftest_wait_timeout", "cmoe_ffn_forward_adapted",
 ]
 
 
@@ -102,6 +102,7 @@ def load() -> C.CDLL:
     lib.cmoe_adapter_forward.argtypes = [vp, vp, i64, vp, i32, vp, vp, i64, vp, i64, vp, vp, i64, vp]
     lib.cmoe_adapter_backward.argtypes = [vp, vp, i64, vp, i64, vp, vp, i32, vp, vp, i64, vp, i64, vp, vp, vp, i64, vp]
     lib.cmoe_adapter_status.argtypes = [C.POINTER(i32), vp]
+    lib.cmoe_adapter_selftest_wait_timeout.argtypes = [i64, vp]
     lib.cmoe_ffn_forward_adapted.argtypes = [vp, vp, i32, vp, vp, vp, vp, i64, vp]
     lib.cmoe_status_string.argtypes = [C.c_int]
     lib.cmoe_status_string.restype = C.c_char_p
@@ -648,6 +649,11 @@ def adapter_status(stream=None) -> int:
     if st not in (0, -6):
         _check(st, "cmoe_adapter_status")
     return w.value
+
+
+def adapter_selftest_wait_timeout(limit_cycles: int = 2_000_000, stream=None) -> None:
+    """cmoe_adapter_selftest_wait_timeout: one warp runs a bounded wait to its limit."""
+    _check(load().cmoe_adapter_selftest_wait_timeout(limit_cycles, _stream_ptr(stream)), "cmoe_adapter_selftest_wait_timeout")
 
 
 def adapter_scratch_bytes(n_adapters: int, rank: int, d_in: int, d_out: int, dtype, n_rows: int, with_row_adapter: bool = True,

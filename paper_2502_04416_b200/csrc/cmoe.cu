@@ -1742,6 +1742,18 @@ int cmoe_adapter_status(int32_t* device_error_word, void* stream) {
   return w ? arg_fail(CMOE_ERR_DEVICE_TIMEOUT, "a bounded device-side wait of an adapter kernel ran out") : CMOE_OK;
 }
 
+int cmoe_adapter_selftest_wait_timeout(int64_t limit_cycles, void* stream) {
+  if (limit_cycles < 1000 || limit_cycles > 2000000000LL)
+    return arg_fail(CMOE_ERR_INVALID_ARG, "limit_cycles outside [1e3, 2e9]");
+  int n_sms = 0;
+  RC_TRY(device_sms(&n_sms));
+  void* word = nullptr;
+  CU_TRY(cudaGetSymbolAddress(&word, g_adapter_error));
+  CU_TRY(launch_kernel(false, wait_timeout_probe_kernel, dim3(1), dim3(32), 0, static_cast<cudaStream_t>(stream), static_cast<int32_t*>(word),
+                       (long long)limit_cycles));
+  return CMOE_OK;
+}
+
 int cmoe_ffn_forward_adapted(cmoe_layer* L, const void* x, int32_t T, const cmoe_adapters* ad, const int32_t* row_adapter,
                              void* out, void* scratch, int64_t scratch_bytes, void* stream) {
   if (!L) return arg_fail(CMOE_ERR_INVALID_ARG, "null layer");
