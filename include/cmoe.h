@@ -473,7 +473,7 @@ int cmoe_adapter_selftest_wait_timeout(int64_t limit_cycles, void* stream);
 
 /* out_t = F_MoE(x_t) + s_a B_a A_a x_t: cmoe_ffn_forward with an adapter per request beside the layer, which all of them share.
  * The adapters' d_in and d_out are the layer's d_model and their dtype is the layer's; x, T, out as in cmoe_ffn_forward,
- * row_adapter, scratch as in cmoe_adapter_forward.  Arguments are checked before anything is launched.  The adapters are not
+ * row_adapter, scratch as in cmoe_adapter_forward.  The layer's device is the current one.  Arguments are checked before anything is launched.  The adapters are not
  * part of the per-stage times; cmoe_layer_launch_count includes their launches.  Errors: those of both calls. */
 int cmoe_ffn_forward_adapted(cmoe_layer* layer, const void* x, int32_t T, const cmoe_adapters* ad, const int32_t* row_adapter,
                              void* out, void* scratch, int64_t scratch_bytes, void* stream);

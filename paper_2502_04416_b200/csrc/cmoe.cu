@@ -1761,6 +1761,9 @@ int cmoe_ffn_forward_adapted(cmoe_layer* L, const void* x, int32_t T, const cmoe
   const int d = L->cfg.d_model;
   if (ad->d_in != d || ad->d_out != d || ad->dtype != L->cfg.dtype)
     return arg_fail(CMOE_ERR_INVALID_ARG, "adapters: d_in, d_out or dtype is not the layer's");
+  int dev = 0;
+  CU_TRY(cudaGetDevice(&dev));
+  if (dev != L->device) return arg_fail(CMOE_ERR_INVALID_ARG, "adapters: the layer belongs to another device than the current one");
   if (T <= 0) return cmoe_ffn_forward(L, x, T, out, stream);
   const Mat mx{x, d, d}, mo{out, d, d};
   RC_TRY(check_adapter_forward(ad, mx, T, mo, mo, nullptr));

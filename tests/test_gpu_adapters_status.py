@@ -1,4 +1,4 @@
-"""-m gpu: what the adapters' calls say after a bounded wait has run out."""
+"""-m gpu: what the adapters' calls say after a bounded wait has run out, and of a layer on another device."""
 import pytest
 
 from paper_2502_04416_b200 import binding
@@ -31,3 +31,18 @@ def test_wait_timeout_is_reported_once_and_calls_go_on():
     for limit in (10, 2_000_000_001):
         with pytest.raises(binding.CmoeError):
             binding.adapter_selftest_wait_timeout(limit)
+
+
+def test_a_layer_on_another_device_is_refused():
+    import torch
+    from paper_2502_04416_b200 import workloads as wl
+    from tests import parity
+    if torch.cuda.device_count() < 2:
+        pytest.skip("one device")
+    inp = wl.make_inputs(wl.Workload("elsewhere", wl.LayerShape(256, 1024, 8, 2, 2, "bf16"), (40,), seed=3))
+    layer = parity.gpu_layer(inp.layers[0], 40)
+    x = parity.to_device(inp.x, "bf16").to("cuda:1")
+    a, b = torch.zeros(1, 8, 256, dtype=torch.bfloat16, device="cuda:1"), torch.zeros(1, 256, 8, dtype=torch.bfloat16, device="cuda:1")
+    with pytest.raises(binding.CmoeError, match="another device"):
+        layer.forward_adapted(x, a, b)
+    layer.destroy()
