@@ -243,21 +243,13 @@ template <typename T> struct AdapterArgs {
 // A 32-bit float as two bf16 whose sum has at least 15 of its significant bits, for twice the MMAs of a narrow product: the error, 2^-16
 // of the value, is below a bf16 result's rounding unless the terms of a sum cancel to less than about 2^-7 of their size; it is stated with
 // the calls.  Neither part is zero unless the value is, and both have its sign, so that a sum that meets an infinity on the
-// other side takes no 0 * Inf from a part: the high part is cut off (it never rounds up to infinity) and, where nothing would be left
-// for the low part, one step smaller.  Infinities and NaN are both parts.  (Values below 2^-103 may lose their low part to the
-// end of the range.)
+// other side takes no 0 * Inf from a part: the high part is the last step strictly below the value's magnitude, which leaves something
+// for the low part.  Of an infinity the low part is one, and of a NaN.  (Values below 2^-103 may lose their low part to the end of the range.)
 __device__ __forceinline__ void split_bf16(float v, uint16_t& hi, uint16_t& lo) {
-  uint32_t u = __float_as_uint(v) & 0xffff0000u;
-  if ((u & 0x7f800000u) == 0x7f800000u) {
-    hi = lo = __bfloat16_as_ushort(__float2bfloat16_rn(v));
-    return;
-  }
-  lo = __bfloat16_as_ushort(__float2bfloat16_rn(v - __uint_as_float(u)));
-  if ((lo & 0x7fffu) == 0u && (u & 0x7fff0000u) > 0x00010000u) {
-    u -= 0x00010000u;
-    lo = __bfloat16_as_ushort(__float2bfloat16_rn(v - __uint_as_float(u)));
-  }
-  hi = (uint16_t)(u >> 16);
+  const uint32_t u = __float_as_uint(v);
+  const uint32_t h = ((max(u & 0x7fffffffu, 1u) - 1u) & 0x7fff0000u) | (u & 0x80000000u);
+  hi = (uint16_t)(h >> 16);
+  lo = __bfloat16_as_ushort(__float2bfloat16_rn(v - __uint_as_float(h)));
 }
 // Transposes an 8 x 8 matrix of 16-bit elements held by the warp (lane 4 i + j: row i, columns 2 j and 2 j + 1).
 __device__ __forceinline__ uint32_t transpose8(uint32_t v) {
