@@ -544,17 +544,19 @@ def dropout(x, drop: Dropout, residual=None, out=None, stream=None):
 def _adapters(dtype, dev: int, a, b, scale) -> CmoeAdapters:
     n, r, d_in = a.shape
     d_out = b.shape[1]
-    if max(n, r, d_in, d_out) > _MOST:
+    if d_in > _MOST or d_out > _MOST:                          # the other two could not be that large in any memory
         raise ValueError(f"a, b: a dimension above {_MOST}")
     code = CMOE_BF16 if dtype is _torch.bfloat16 else CMOE_FP32 if dtype is _torch.float32 else None
     if code is None:
         raise TypeError(f"unsupported dtype {dtype}")
     s_ptr = None if scale is None else _like(scale, "scale", (n,), _torch.float32, dev)
+    copy = None
     if s_ptr is not None and s_ptr & 7:                        # a slice of a larger set may start anywhere: the call takes it on 8 bytes
-        scale = scale.clone()
-        s_ptr = scale.data_ptr()
+        copy = scale.clone()
+        s_ptr = copy.data_ptr()
     ad = CmoeAdapters(n, r, d_in, d_out, code, _like(a, "a", (n, r, d_in), dtype, dev), _like(b, "b", (n, d_out, r), dtype, dev), s_ptr)
-    ad.scale_tensor = scale                                    # lives as long as the struct that has its address
+    if copy is not None:
+        ad.scale_copy = copy                                   # lives as long as the struct that has its address
     return ad
 
 
