@@ -69,3 +69,33 @@ def test_every_nan_of_z_is_one(rows, r):
     assert gb[0, :, 5].isnan().all() and not ga.isnan().any()
     rest = [i for i in range(r) if i != 5]
     assert not gb[0][:, rest].isnan().any()
+
+
+@pytest.mark.parametrize("dtype,rows,n,r,with_ids", SHAPES + [("bf16", 1, 1, 8, False), ("fp32", 1100, 3, 64, True)])
+@pytest.mark.parametrize("where", ["x", "base"])
+def test_a_rows_own_infinities(dtype, rows, n, r, with_ids, where):
+    """The forward: an infinity or a NaN of a row goes through both products as the formulas have it, into z and out."""
+    import torch
+    d_in, d_out = 72, 136
+    rng = np.random.default_rng(rows + r)
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    v = dict(x=np.zeros((rows, d_in)), a=_whole(rng, (n, r, d_in), 2), b=_whole(rng, (n, d_out, r), 2), base=_whole(rng, (rows, d_out), 3))
+    v["x"][np.arange(rows), rng.integers(0, d_in, rows)] = _whole(rng, rows, 3)
+    ids = rng.integers(0, n, rows) if with_ids else np.zeros(rows, dtype=np.int64)
+    for i, t in enumerate(rng.choice(rows, min(rows, 6), replace=False)):
+        v[where][t, rng.integers(0, v[where].shape[1])] = [np.inf, -np.inf, np.inf, -np.inf, np.nan, np.inf][i]
+    v["b"][:, ::3] = np.abs(v["b"][:, ::3])                  # some columns where no two infinities of other signs meet
+    v["a"] = np.abs(v["a"])
+    dev = {k: torch.from_numpy(t).cuda().to(dt) for k, t in v.items()}
+    out, z = binding.adapter_forward(dev["x"], dev["a"], dev["b"], torch.from_numpy(ids.astype(np.int32)).cuda() if with_ids else None,
+                                     base=dev["base"], want_z=True)
+    with np.errstate(invalid="ignore"):
+        want_z = np.stack([(v["a"][k] * v["x"][t]).sum(1) for t, k in enumerate(ids)])
+        want = np.stack([v["base"][t] + (v["b"][k] * want_z[t]).sum(1) for t, k in enumerate(ids)])
+        assert np.isinf(want).any()
+        for g, w, half in ((out, want, torch.finfo(dt).eps / 2), (z, want_z, 0.0)):
+            g = g.double().cpu().numpy()
+            np.testing.assert_array_equal(np.isnan(g), np.isnan(w))
+            np.testing.assert_array_equal(g[np.isinf(w)], w[np.isinf(w)])
+            ok = np.isfinite(w)
+            assert (np.abs(g[ok] - w[ok]) <= half * np.abs(w[ok])).all()
