@@ -1241,6 +1241,9 @@ inline bool adapter_small(const int32_t* row_adapter, int n_rows, bool backward)
 // kernels of a call, 4096 + 4096 columns (rows x adapters, rank): forward 1024 x 1, 64: 19 against 23; 512 x 1, 64: 20, 16;
 // 2048 x 64, 64: 53, 67; 8192 x 16, 64: 54, 109; 8192 x 16, 32: 53, 77; 4096 x 64, 32: 52, 66; 2048 x 1, 32: 26, 21; 8192 x 8, 16:
 // 53, 51.  Gradients 8192 x 16, 64: 104, 191; 1024 x 16, 64: 69, 87; 2048 x 1, 64: 53, 52; 8192 x 16, 32: 118, 146; 2048 x 64, 32: 183, 150.
+// The rule does not ask for the widths.  Narrow layers are small either way and lose some microseconds to the exchange: 1024 + 1024 columns
+// (rows x adapters, rank) forward 1024 x 1, 64: 11.3, 9.8; 8192 x 1, 64: 15.7, 22.1; 4096 x 64, 32: 23.6, 16.4; gradients 1024 x 16, 64: 33, 29;
+// 16384 x 64, 64: 75, 124; 256 + 256 columns forward 1024 x 1, 64: 10.1, 7.0; 8192 x 16, 32: 16.5, 13.2; 16384 x 64, 64: 17.7, 25.6.
 constexpr int kAdTallRows = 128;
 inline bool adapter_tall(bool bf, int n_rows, int n, int r, bool small) {
   return bf && !small && (r > 32 ? n_rows >= 1024 && n_rows >= 32 * n : r > 16 && n_rows >= 4096 && n_rows >= 64 * n);

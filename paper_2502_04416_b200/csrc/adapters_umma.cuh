@@ -671,8 +671,18 @@ inline cudaError_t launch_outer_umma(OuterArgs p, int n_sms, bool dep, cudaStrea
   int ctas = 1;
   while (ctas < 8 && (long long)slices * p.n * ctas * 2 < 3LL * n_sms && p.n_rows / p.n >= 512 * ctas) ctas *= 2;
   // Rows of several adapters are seldom shared evenly: two adapters that have nearly all of them should fill the SMs as well, where
-  // there are enough of them to pay for more blocks (by 2 and 4 blocks, 16384 rows in random shares of four adapters: 102, 95 us;
-  // by 1 and 2, 8192 rows of eight adapters, 4096 + 4096: random shares 64, 50, even ones 38, 50).
+  // there are enough of them to pay for more blocks.  The whole gradient by the split above and by twice as many blocks, us, for even shares,
+  // random ones and 90 % of the rows with one adapter (rank 64, 5120 + 5120 columns / 4096 + 4096).  From 2048 rows a block on:
+  //   16384 x 4   210, 209; 206, 193; 253, 192 / 146, 161; 189, 164; 236, 172
+  //   24000 x 4   315, 305; 309, 294; 381, 292 / 222, 239; 263, 248; 356, 262
+  //   16384 x 8   212, 205; 211, 191; 384, 253 / 148, 160; 193, 163; 368, 235
+  //   32768 x 16  367, 372; 389, 379; 750, 485 / 288, 314; 328, 321; 718, 452
+  // and below, where the split stays as it is:
+  //   12000 x 4   192, 198; 189, 185; 219, 177 / 132, 148; 159, 150; 197, 152
+  //    8192 x 8   129, 132; 136, 130; 211, 146 /  92, 105; 122, 113; 202, 136
+  //   16384 x 16  208, 220; 203, 212; 387, 258 / 163, 184; 170, 180; 372, 240
+  // A doubling costs even shares up to 10 % above and 16 % below (two of them 20 %: 32768 x 8, 4096 + 4096 columns, 268, 321); random ones
+  // gain 2 to 16 % above, and below between 8 % and -6 %.
   while (p.n > 1 && ctas < 8 && 4LL * slices * ctas < 3LL * n_sms && p.n_rows / p.n >= 2048 * ctas) ctas *= 2;
   const dim3 grid(slices, p.n, ctas), cl(1, 1, ctas);
   return p.drop.thr16 ? launch_cluster(dep, adapter_outer_umma_kernel<true>, grid, cl, kAgSmem, kAgSmem, st, p, kAuThreads)
