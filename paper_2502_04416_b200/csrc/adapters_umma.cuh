@@ -110,7 +110,7 @@ adapter_umma_kernel(const AdapterArgs<bf16> p) {
   }
   tc_fence_before();
   __syncthreads();
-  grid_dep_trigger();                                                          // this block has its tensor memory (see the header)
+  grid_dep_trigger();                                                          // this block has its tensor memory (see the top of the file)
   rc_cluster_arrive();
   rc_cluster_wait();                                                           // every peer's barriers are there
   tc_fence_after();
